@@ -1,7 +1,7 @@
 """Thin ctypes binding of libqp_hip.so: argument marshalling only.
 
 Every function has the name and argument order of its C-ABI counterpart in include/qp.h
-(the path) or include/qp_layer.h (the decoder layer around it) and takes torch tensors on the GPU (device memory and streams are all torch is used for).
+(the path), include/qp_layer.h (the decoder layer around it) or include/qp_paged.h (the paged cache) and takes torch tensors on the GPU (device memory and streams are all torch is used for).
 There is no CPU fallback: if the library is missing, loading raises.
 """
 from __future__ import annotations
@@ -54,6 +54,22 @@ class qp_layer_weights(ctypes.Structure):
                 ("ln1_w", "w_qkv", "b_qkv", "w_o", "ln2_w", "w_gate_up", "w_down")]
 
 
+class qp_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class qp_paged_batch(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class qp_paged_plan_info(ctypes.Structure):
+    _fields_ = [("rows_per_tile", ctypes.c_int32), ("key_chunks", ctypes.c_int32), ("chunk_entries", ctypes.c_int32),
+                ("workgroups", ctypes.c_int32), ("scratch_bytes", ctypes.c_size_t)]
+
+
 class qp_feed_stats(ctypes.Structure):
     _fields_ = [("groups", ctypes.c_int32), ("total_ms", ctypes.c_double), ("waited_ms", ctypes.c_double),
                 ("first_group_wait_ms", ctypes.c_double)]
@@ -79,6 +95,7 @@ class QPError(RuntimeError):
 _lib = None
 _vp, _i32, _i64, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 _LP, _CP = ctypes.POINTER(qp_layout), ctypes.POINTER(qp_cache)
+_PC, _PB = ctypes.POINTER(qp_paged_cache), ctypes.POINTER(qp_paged_batch)
 _SP, _WP, _f32 = ctypes.POINTER(qp_layer_shape), ctypes.POINTER(qp_layer_weights), ctypes.c_float
 
 SIGNATURES = {
@@ -111,6 +128,13 @@ SIGNATURES = {
     "qp_layer_group": (_i32, [_LP, _SP, _WP, _vp, _vp, _i64, _i32, _i32, _vp, _i32, _i32, _i32, _CP, _vp, _vp, _vp,
                               _sz, _vp]),
     "qp_layer_window_queries": (_i32, [_LP, _SP, _WP, _vp, _vp, _i64, _i32, _vp, _vp, _sz, _vp]),
+    # include/qp_paged.h
+    "qp_paged_workspace_bytes": (_sz, [_LP, _i32, _i32, _i32, _i32, _i32]),
+    "qp_paged_append": (_i32, [_LP, _PC, _PB, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _vp]),
+    "qp_paged_attend": (_i32, [_LP, _PC, _PB, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "qp_paged_weigh": (_i32, [_LP, _PC, _PB, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "qp_paged_evict": (_i32, [_LP, _PC, _PB, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "qp_paged_plan": (_i32, [_LP, _PC, _PB, _sz, ctypes.POINTER(qp_paged_plan_info)]),
     # include/qp_feed.h
     "qp_feed_create": (_i32, [_i32, _sz, _i32, ctypes.POINTER(_vp)]),
     "qp_feed_destroy": (None, [_vp]),
@@ -462,3 +486,152 @@ class Feed:
         ms = ctypes.c_double()
         _check(lib().qp_feed_stub_join(self.h, ctypes.byref(ms)), "qp_feed_stub_join")
         return ms.value
+
+
+# ---- the paged cache (include/qp_paged.h) ----
+
+def _on_device(*tensors):
+    """Calls run on the current device: a tensor of another one would be read across the link, or not at all."""
+    here = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("expected tensors of the current GPU")
+
+
+def _typed(t, dtype, shape, name):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _layout_dtype(layout):
+    return torch.float32 if layout.dtype == QP_F32 else torch.bfloat16
+
+
+class PagedCache:
+    """Owner of the device buffers behind a qp_paged_cache: a pool of pages that many sequences share."""
+
+    def __init__(self, layout: qp_layout, n_pages: int, page_tokens: int, device="cuda", fmt=QP_CACHE_SAME, weights=True,
+                 k=None, v=None, pos=None, weight=None):
+        """New zeroed buffers (positions -1), or the caller's own: k, v [n_pages][H_kv][page_tokens][d] in the layout's dtype
+        or torch.float8_e4m3fn, pos int32 and weight float32 [n_pages][H_kv][page_tokens]. weights=False: a pool without them,
+        which paged_weigh and paged_evict refuse."""
+        rows = (n_pages, layout.n_kv_heads, page_tokens)
+        if k is not None and k.dtype == torch.float8_e4m3fn:
+            fmt = QP_CACHE_FP8_E4M3
+        dt = torch.float8_e4m3fn if fmt == QP_CACHE_FP8_E4M3 else _layout_dtype(layout)
+        new = lambda t, shape, dtype, name: torch.zeros(shape, dtype=dtype, device=device) if t is None else _typed(t, dtype, shape, name)
+        self.k = new(k, (*rows, layout.head_dim), dt, "k")
+        self.v = new(v, (*rows, layout.head_dim), dt, "v")
+        self.pos = torch.full(rows, -1, dtype=torch.int32, device=device) if pos is None else _typed(pos, torch.int32, rows, "pos")
+        self.weight = new(weight, rows, torch.float32, "weight") if weights or weight is not None else None
+        _on_device(self.k, self.v, self.pos, self.weight)
+        self.c = qp_paged_cache(_ptr(self.k), _ptr(self.v), _ptr(self.pos), _ptr(self.weight), n_pages, page_tokens, fmt)
+
+
+class PagedBatch:
+    """The sequences of a call: page_table int32 [n_seqs][pages], length int32 [n_seqs] and row_start int32 [n_seqs + 1] on the
+    GPU (their values may change between calls, and between replays of a captured one). max_new and max_len bound what is
+    launched; by default every row may belong to one sequence, and a sequence may fill its table."""
+
+    def __init__(self, page_table, length, row_start=None, n_rows=0, max_new=None, max_len=None):
+        if page_table.dim() != 2 or page_table.dtype != torch.int32:
+            raise ValueError("page_table: expected int32 [n_seqs][pages]")
+        n_seqs = page_table.shape[0]
+        _typed(length, torch.int32, (n_seqs,), "length")
+        if row_start is not None:
+            _typed(row_start, torch.int32, (n_seqs + 1,), "row_start")
+        _on_device(page_table, length, row_start)
+        self.page_table, self.length, self.row_start, self.max_len = page_table, length, row_start, max_len
+        self.c = qp_paged_batch(_ptr(page_table), _ptr(length), _ptr(row_start), n_seqs, page_table.shape[1], n_rows,
+                                n_rows if max_new is None else max_new, 0)
+
+    def of(self, page_tokens):
+        """The struct for a pool of such pages."""
+        most = min(self.c.table_pages * page_tokens, 1 << 30)
+        self.c.max_len = most if self.max_len is None else self.max_len
+        return ctypes.byref(self.c)
+
+
+def paged_workspace_bytes(layout, n_seqs, n_rows, max_new, max_len, keep=0) -> int:
+    return lib().qp_paged_workspace_bytes(ctypes.byref(layout), n_seqs, n_rows, max_new, max_len, keep)
+
+
+def make_paged_workspace(layout, batch: PagedBatch, keep=0, page_tokens=256, device="cuda") -> torch.Tensor:
+    """Scratch for every paged call of the batch's sizes (page_tokens: needed where the batch states no max_len)."""
+    batch.of(page_tokens)
+    n = paged_workspace_bytes(layout, batch.c.n_seqs, batch.c.n_rows, batch.c.max_new, batch.c.max_len, keep)
+    if n == 0:
+        raise QPError(QP_ERR_INVALID_ARG, "qp_paged_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _rows_of(layout, batch, q, heads, name):
+    return _typed(q, _layout_dtype(layout), (batch.c.n_rows, heads, layout.head_dim), name)
+
+
+def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
+    """k, v [n_rows][H_kv][d] of any strides whose rows are runs of d elements (a flat cache's [H_kv][capacity][d] comes as
+    k.transpose(0, 1)[:n]); pos int32 [n_rows], or [n_rows][H_kv] with a position per head. Rows of an 8-bit pool may be
+    torch.float8_e4m3fn already."""
+    raw = k.dtype == torch.float8_e4m3fn
+    shape = (batch.c.n_rows, layout.n_kv_heads, layout.head_dim)
+    dt = torch.float8_e4m3fn if raw else _layout_dtype(layout)
+    _typed(k, dt, shape, "k")
+    _typed(v, dt, shape, "v")
+    _on_device(k, v, pos, cache.k, batch.page_table)
+    steps = [tuple(0 if n == 1 else x for n, x in zip(shape, t.stride())) for t in (k, v)]  # of one row, any stride does
+    if steps[0] != steps[1] or steps[0][2] != 1:
+        raise ValueError("k and v: expected the same strides and rows in one run")
+    if pos.dtype != torch.int32 or tuple(pos.shape) not in (shape[:1], shape[:2]):
+        raise ValueError("pos: expected int32 [n_rows] or [n_rows][H_kv]")
+    st = lib().qp_paged_append(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), k.data_ptr(),
+                               v.data_ptr(), steps[0][0], steps[0][1], pos.data_ptr(), pos.stride(0),
+                               pos.stride(1) if pos.dim() == 2 else 0, QP_CACHE_FP8_E4M3 if raw else QP_CACHE_SAME, _stream())
+    _check(st, "qp_paged_append")
+
+
+def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None, workspace=None):
+    """q, out [n_rows][H_q][d], lse float32 [H_q][n_rows]."""
+    _rows_of(layout, batch, q, layout.n_q_heads, "q")
+    _rows_of(layout, batch, out, layout.n_q_heads, "out")
+    if lse is not None:
+        _typed(lse, torch.float32, (layout.n_q_heads, batch.c.n_rows), "lse")
+    _on_device(q, out, lse, workspace, cache.k, batch.page_table)
+    wp, wb = _ws(workspace)
+    st = lib().qp_paged_attend(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), _ptr(q), _ptr(out),
+                               _ptr(lse), wp, wb, _stream())
+    _check(st, "qp_paged_attend")
+
+
+def paged_weigh(layout, cache: PagedCache, batch: PagedBatch, q, lse, accumulate=True, workspace=None):
+    """Adds to (or, accumulate=False, writes) cache.weight what the batch's rows of paged_attend's lse looked at."""
+    _rows_of(layout, batch, q, layout.n_q_heads, "q")
+    _typed(lse, torch.float32, (layout.n_q_heads, batch.c.n_rows), "lse")
+    _on_device(q, lse, workspace, cache.k, batch.page_table)
+    wp, wb = _ws(workspace)
+    st = lib().qp_paged_weigh(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), _ptr(q), _ptr(lse),
+                              int(accumulate), wp, wb, _stream())
+    _check(st, "qp_paged_weigh")
+
+
+def paged_evict(layout, cache: PagedCache, batch: PagedBatch, keep, n_first, n_last, to_table, to_len, kept=None, workspace=None):
+    """to_table int32 [n_seqs][pages], to_len int32 [n_seqs], kept int32 [n_seqs][H_kv][keep] or None."""
+    n_seqs = batch.c.n_seqs
+    if to_table.dim() != 2 or to_table.dtype != torch.int32 or to_table.shape[0] != n_seqs:
+        raise ValueError("to_table: expected int32 [n_seqs][pages]")
+    _typed(to_len, torch.int32, (n_seqs,), "to_len")
+    if kept is not None:
+        _typed(kept, torch.int32, (n_seqs, layout.n_kv_heads, keep), "kept")
+    _on_device(to_table, to_len, kept, workspace, cache.k, batch.page_table)
+    wp, wb = _ws(workspace)
+    st = lib().qp_paged_evict(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), keep, n_first, n_last,
+                              _ptr(to_table), to_table.shape[1], _ptr(to_len), _ptr(kept), wp, wb, _stream())
+    _check(st, "qp_paged_evict")
+
+
+def paged_plan(layout, cache: PagedCache, batch: PagedBatch, workspace_bytes=0) -> dict:
+    info = qp_paged_plan_info()
+    _check(lib().qp_paged_plan(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), workspace_bytes,
+                               ctypes.byref(info)), "qp_paged_plan")
+    return {name: getattr(info, name) for name, _ in qp_paged_plan_info._fields_}

@@ -10,17 +10,7 @@
 // ranked directly by topk_rank_kernel.
 //
 // Selection = find the k-th largest key T and how many keys equal to T survive (`need`), then emit.
-//   * While loading, the workgroup takes the minimum and maximum key. A round spreads the current key
-//     range [lo, lo+span] over up to 2048 buckets of equal power-of-two width (bucket = (key-lo) >> sh),
-//     counts keys per bucket with LDS atomics, turns the counts into suffix sums (two buckets per
-//     thread, shuffles inside a wavefront, 16 wavefront totals through LDS) and picks the bucket in
-//     which the k-th largest key falls; the range shrinks to that bucket. Because the buckets follow the
-//     data's own range, real scores (which share sign and exponent) spread over them and the atomics
-//     rarely collide; one ballot per batch folds a digit shared by many lanes into a single atomic, so
-//     that a constant score vector does not serialise either.
-//   * As soon as the bucket holds at most 256 keys they are copied to a list and ranked directly
-//     (every candidate counts the candidates above and equal to it). Otherwise another round runs on the
-//     bucket; a bucket of width one is exact. The width shrinks by 2^11 per round: at most 3 rounds.
+//   * While loading, the workgroup takes the minimum and maximum key; select_threshold (select.h) narrows that range to T.
 //   * Emit: a token survives iff key > T, or key == T and fewer than `need` equal keys precede it: ties go to
 //     the lower index and the kept list comes out in ascending token order. The workgroup counts the
 //     (greater, equal) keys before its slice, which fixes where the slice's survivors start; inside the slice
@@ -28,28 +18,17 @@
 //     inside the batch, running counts its slot.
 #include "append.h"
 #include "qp_internal.h"
+#include "select.h"
 
 namespace qp {
 
-constexpr int TOPK_THREADS = 1024;
+constexpr int TOPK_THREADS = SEL_THREADS;
 constexpr int TOPK_WAVES = TOPK_THREADS / 64;
-constexpr int SEL_BITS = 11;
-constexpr int SEL_NB = 1 << SEL_BITS;  // buckets per round, two per thread
-constexpr int SEL_LIST = 256;          // a bucket of at most this many keys is ranked directly
-constexpr int SEL_UNROLL = 2;          // independent LDS reads per thread and loop trip
 constexpr int LOAD_UNROLL = 8;         // score loads per thread in flight while the keys are brought in
-constexpr int SEL_MAX_ROUNDS = 4;      // 3 suffice for 32-bit keys; the bound makes termination explicit
 constexpr int GATHER_UNROLL = 4;       // rows per lane group in flight in the copy
 constexpr int SLICE_MAX = 4096;        // tokens per slice at most (their survivors' indices sit in LDS)
 constexpr int SLICE_WANT_KEEP = 128;   // survivors per slice aimed for
 constexpr int SLICES_MAX = 16;
-static_assert(SEL_NB == 2 * TOPK_THREADS, "two buckets per thread");
-
-__device__ __forceinline__ uint32_t order_key(float s) {
-  s += 0.f;  // -0.0 -> +0.0 so that the two zeros tie
-  const uint32_t u = __float_as_uint(s);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // ascending in s
-}
 
 // Turns the arguments of a run into those of this workgroup's group (grid.z).
 __device__ __forceinline__ void run_group(TopkArgs& a, size_t token_bytes) {
@@ -94,10 +73,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_all_kernel(TopkArgs a, 
 template <typename T, int D>
 __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, int32_t* __restrict__ kept_out, int slice_tokens) {
   extern __shared__ uint32_t keys[];  // [n_g] keys, then [slice_tokens] kept token indices of this slice
-  __shared__ __attribute__((aligned(8))) uint32_t hist[SEL_NB];
-  __shared__ uint32_t list[SEL_LIST];
-  __shared__ uint32_t wave_a[TOPK_WAVES], wave_b[TOPK_WAVES], wave_min[TOPK_WAVES], wave_max[TOPK_WAVES];
-  __shared__ uint32_t sel_bucket, sel_need, sel_count, sel_key, list_n;
+  __shared__ SelectLds lds;
+  __shared__ uint32_t wave_b[TOPK_WAVES], wave_min[TOPK_WAVES], wave_max[TOPK_WAVES];
 
   run_group(a, (size_t)a.h_kv * D * sizeof(T));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -127,9 +104,9 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
     wave_min[wave] = kmin;
     wave_max[wave] = kmax;
   }
-  hist[2 * tid] = 0;
-  hist[2 * tid + 1] = 0;
-  if (tid == 0) list_n = 0;
+  lds.hist[2 * tid] = 0;
+  lds.hist[2 * tid + 1] = 0;
+  if (tid == 0) lds.list_n = 0;
   __syncthreads();
   uint32_t lo = 0xffffffffu, hi = 0u;
 #pragma unroll
@@ -138,100 +115,8 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
     hi = max(hi, wave_max[w]);
   }
 
-  const int n_round = (n + TOPK_THREADS - 1) / TOPK_THREADS * TOPK_THREADS;  // whole wavefronts take part
-  uint32_t span = hi - lo;          // keys still in play: lo <= key <= lo + span
-  uint32_t need = (uint32_t)a.keep; // rank of T among them, counted from the largest
-  uint32_t thr = lo;
-  for (int round = 0; round < SEL_MAX_ROUNDS; ++round) {
-    const int bits = span ? 32 - __builtin_clz(span) : 0;
-    const int sh = bits > SEL_BITS ? bits - SEL_BITS : 0;
-    for (int j0 = tid; j0 < n_round; j0 += SEL_UNROLL * TOPK_THREADS) {
-      uint32_t kk[SEL_UNROLL];
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) kk[u] = j0 + u * TOPK_THREADS < n ? keys[j0 + u * TOPK_THREADS] : 0u;
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) {
-        const int j = j0 + u * TOPK_THREADS;  // j >= n_round only when j >= n: such a batch has no active lane
-        const uint32_t off = kk[u] - lo;
-        bool act = j < n && off <= span;  // a key below lo wraps to a large offset
-        const uint32_t bin = off >> sh;
-        const unsigned long long am = __ballot(act);
-        if (am != 0) {  // fold the first active lane's bucket when many lanes share it
-          const int leader = __ffsll((long long)am) - 1;
-          const uint32_t b0 = (uint32_t)__builtin_amdgcn_readlane((int)bin, leader);
-          const bool mine = act && bin == b0;
-          const unsigned long long same = __ballot(mine);
-          if (__popcll(same) >= 8) {
-            if (lane == leader) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
-            if (mine) act = false;
-          }
-        }
-        if (act) atomicAdd(&hist[bin], 1u);
-      }
-    }
-    __syncthreads();
-    // suffix sums over the buckets: this thread owns buckets 2 tid and 2 tid + 1 (and clears them for a next round)
-    const uint2 hb = *(const uint2*)&hist[2 * tid];
-    *(uint2*)&hist[2 * tid] = make_uint2(0u, 0u);
-    const uint32_t own = hb.x + hb.y;
-    uint32_t suf = own;  // inclusive suffix over the wavefront's lanes
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t t = __shfl_down(suf, o, 64);
-      if (lane + o < 64) suf += t;
-    }
-    if (lane == 0) wave_a[wave] = suf;
-    __syncthreads();
-    uint32_t above = suf - own;  // keys in buckets above 2 tid + 1
-#pragma unroll
-    for (int w = 1; w < TOPK_WAVES; ++w) above += w > wave ? wave_a[w] : 0u;
-    const uint32_t suf1 = above + hb.y, suf0 = suf1 + hb.x;
-    if (suf1 >= need && above < need) {  // exactly one (thread, bucket) holds the crossing
-      sel_bucket = 2 * tid + 1;
-      sel_need = need - above;
-      sel_count = hb.y;
-    } else if (suf0 >= need && suf1 < need) {
-      sel_bucket = 2 * tid;
-      sel_need = need - suf1;
-      sel_count = hb.x;
-    }
-    __syncthreads();
-    const uint32_t first = sel_bucket << sh;  // offset of the chosen bucket's first key
-    need = sel_need;
-    const uint32_t count = sel_count;
-    lo += first;
-    span = min(span - first, (sh ? (1u << sh) : 1u) - 1u);
-    thr = lo;
-    if (sh == 0) break;  // buckets were single keys: T = lo, `need` of its copies survive
-    if (count <= SEL_LIST) {
-      // rank the bucket's keys directly
-      for (int j = tid; j < n; j += TOPK_THREADS) {
-        const uint32_t key = keys[j];
-        if (key - lo <= span) {
-          const uint32_t p = atomicAdd(&list_n, 1u);
-          if (p < (uint32_t)SEL_LIST) list[p] = key;  // always true: the bucket holds `count` keys
-        }
-      }
-      __syncthreads();
-      if (tid < (int)count) {
-        const uint32_t x = list[tid];
-        uint32_t g = 0, e = 0;
-        for (uint32_t m = 0; m < count; ++m) {
-          const uint32_t y = list[m];
-          g += y > x;
-          e += y == x;
-        }
-        if (g < need && need <= g + e) {  // equal candidates write the same values
-          sel_key = x;
-          sel_need = need - g;
-        }
-      }
-      __syncthreads();
-      thr = sel_key;
-      need = sel_need;
-      break;
-    }
-  }
+  uint32_t thr, need;
+  select_threshold([&](int j) { return keys[j]; }, n, lo, hi, (uint32_t)a.keep, lds, thr, need);
   // thr: the k-th largest key; need: how many keys equal to it survive (>= 1)
 
   // this workgroup's slice of the tokens, and the (greater, equal) keys before it
@@ -264,7 +149,7 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
   }
   __syncthreads();  // wave_a / wave_b of the threshold search are free again
   if (lane == 0) {
-    wave_a[wave] = gt_w;
+    lds.wave_a[wave] = gt_w;
     wave_b[wave] = eq_w;
     wave_min[wave] = gt_c;  // the counts before the slice, per wavefront
     wave_max[wave] = eq_c;
@@ -275,9 +160,9 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
   for (int w = 0; w < TOPK_WAVES; ++w) {
     gt_before += wave_min[w];
     eq_before += wave_max[w];
-    gt_run += w < wave ? wave_a[w] : 0u;
+    gt_run += w < wave ? lds.wave_a[w] : 0u;
     eq_run += w < wave ? wave_b[w] : 0u;
-    gt_slice += wave_a[w];
+    gt_slice += lds.wave_a[w];
     eq_slice += wave_b[w];
   }
   const uint32_t out_base = gt_before + min(eq_before, need);  // slot of the slice's first survivor

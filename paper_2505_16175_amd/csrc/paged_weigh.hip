@@ -1,11 +1,14 @@
 // The attention weight that the paged cache's entries received: w[j] (+)= sum over rows of exp2(c q.k_j - lse2), the column sums
-// of the softmax whose row statistics qp_paged_attend left.
+// of the softmax whose row statistics qp_paged_attend left. No atomics: an entry's sum is one lane's, from the first row to the last.
 //
-// A wavefront owns 64 entries (32 of f32) of a KV head, whose keys stay in registers, and walks the sequence's rows 16 at a time:
-// S = Q K^T leaves a lane with one entry (column) and four rows, so the sum over rows stays in the lane until the end, and no
-// two wavefronts meet in an entry: nothing to merge, no atomics. Few rows: bound by the keys' way from HBM, all of which is
-// requested at once. Many rows: bound by the vector unit, 24 cycles per 64 pairs (an exponential, a multiply-add, an add)
-// beside the products' 16.
+// paged_weigh_kernel: few rows (decoding, drafted tokens), and layouts without a tile kernel. A wavefront owns 64 entries (32 of
+// f32) of a KV head, whose keys stay in registers, and walks the sequence's rows 16 at a time: S = Q K^T leaves a lane with one
+// entry (column) and four rows. Bound by the keys' way from HBM, all of which is requested at once.
+//
+// weigh_tile_kernel: chunks over bf16 heads of 128. Four wavefronts own 64 entries each, keys in registers, and walk the rows 32 at a
+// time, which all of them read from LDS: tiles of queries go global -> LDS directly (XOR-swizzled 16-byte chunks), in a ring of four
+// slots, three ahead, one barrier each. Bound by the vector unit: a pair costs a multiply-add, an exponential at a quarter of the
+// rate and an add, 24 cycles per 64 pairs, beside the products' 16 on the matrix pipe.
 #include "paged_rows.h"
 
 #include <algorithm>
@@ -97,7 +100,265 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
   }
 }
 
-size_t paged_weigh_workspace_bytes(int, int, int, int, int) { return 0; }
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+
+constexpr int WT_NW = 4;                 // wavefronts of a workgroup
+constexpr int WT_KEYS = WT_NW * 64;      // and its entries
+constexpr int WT_SLOTS = 4;
+constexpr int WT_TILE = 32 * 256;        // bytes of 32 rows of queries
+constexpr int WT_ROWS = 4096;            // rows whose statistics lie in LDS at a time
+constexpr int WT_LDS = WT_SLOTS * WT_TILE;
+constexpr int WT_MIN_TILES = 8;          // row tiles that a workgroup takes at least where rows are dealt to several
+
+struct WeighTiles {
+  const void* q;
+  const float* lse;
+  int accumulate;
+  int splits;        // workgroups that share a block of entries' rows
+  float* partial;    // [splits][n_seqs][h_kv][max_len], splits > 1
+};
+
+template <int N>
+__device__ __forceinline__ void weigh_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+template <bool F8>
+__global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, WeighTiles o) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ __attribute__((aligned(16))) float neg[WT_ROWS];  // -lse of the segment's rows, base 2
+  __shared__ int dead[WT_ROWS / 32];                           // a row of the tile saw nothing
+  constexpr int ROWB = F8 ? 128 : 256;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int x = blockIdx.x;
+  const int h = x % a.h_kv;
+  x /= a.h_kv;
+  const int s = x % a.n_seqs;
+  x /= a.n_seqs;
+  const int split = x % o.splits;
+  const long long wg_first = (long long)(x / o.splits) * WT_KEYS;
+  const PagedSeq q = paged_seq_of(a, s);
+  if (wg_first >= q.len) return;
+  const int wg_key = (int)wg_first, key0 = wg_key + 64 * wave;
+  const int r_heads = a.h_q / a.h_kv;
+  const int rows = q.n * r_heads;
+  const int mask = (1 << a.page_shift) - 1;
+
+  // this lane's two entries: their keys, and the first row that sees them
+  pr_u32x4 k[2][8];
+  size_t at[2];
+  bool here[2];
+  int first_row[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int key = key0 + 32 * b + l32, kc = min(key, q.len - 1);
+    const int page = a.table[(size_t)s * a.table_pages + (kc >> a.page_shift)];
+    const bool ok = paged_page_ok(page, a.n_pages);
+    here[b] = ok && key < q.len;
+    at[b] = paged_row(ok ? page : 0, h, kc & mask, a.h_kv, a.page_shift);
+    first_row[b] = paged_clamp(key - q.base, 0, q.n) * r_heads;
+    const unsigned char* p = (const unsigned char*)a.k + at[b] * ROWB;
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {
+      if constexpr (F8) {
+        const uint2 raw = *(const uint2*)(p + 16 * st + 8 * g);
+        k[b][st] = pr_widen8(raw.x, raw.y);
+      } else {
+        k[b][st] = *(const pr_u32x4*)(p + 32 * st + 16 * g);
+      }
+    }
+  }
+  // rows from the first tile that sees the workgroup's first entry on, this workgroup's share of them
+  const int tile_first = paged_clamp(wg_key - q.base, 0, q.n) * r_heads / 32, tile_end = (rows + 31) / 32;
+  const int per = (tile_end - tile_first + o.splits - 1) / o.splits;
+  const int begin = min(tile_first + split * per, tile_end), end = min(begin + per, tile_end);
+  const int masked_below = paged_clamp(key0 + 63 - q.base, 0, q.n) * r_heads;  // rows below do not see all of the wavefront's entries
+
+  int q_addr[8];  // query fragment of step st: row l32, chunk 2 st + g at position (2 st + g) ^ (l32 & 15)
+#pragma unroll
+  for (int st = 0; st < 8; ++st) q_addr[st] = l32 * 256 + (((2 * st + g) ^ (l32 & 15)) << 4);
+  const unsigned ring = lds_address(smem);
+  const float c2 = a.scale_log2;
+  float sum[2] = {0.f, 0.f};
+
+  for (int seg = begin; seg < end; seg += WT_ROWS / 32) {  // tiles of a segment
+    const int seg_end = min(end, seg + WT_ROWS / 32);
+    const int row0 = seg * 32;
+    __syncthreads();  // the last segment's statistics and slots have been read
+    if (tid < WT_ROWS / 32) dead[tid] = 0;
+    __syncthreads();
+    for (int r = tid; r < (seg_end - seg) * 32; r += WT_NW * 64) {
+      float v = -INFINITY;
+      if (row0 + r < rows) {
+        const int t = (row0 + r) / r_heads, j = row0 + r - t * r_heads;
+        const float z = o.lse[(size_t)(h * r_heads + j) * a.n_rows + q.row0 + t];
+        v = -z * 1.4426950408889634f;
+        if (z == -INFINITY) {
+          v = -INFINITY;
+          dead[r >> 5] = 1;
+        }
+      }
+      neg[r] = v;
+    }
+    // queries: request i of a wavefront fills rows 8 wave + 4 i + (lane >> 4) of a slot, chunk lane & 15 of each from where the swizzle
+    // has it; a row's offset goes on by 32 rows from tile to tile
+    const int t_seg = row0 / r_heads;
+    const unsigned char* const qb = (const unsigned char*)o.q + ((size_t)(q.row0 + t_seg) * a.h_q + (size_t)h * r_heads) * 256;
+    const int last_row = min(rows, seg_end * 32) - 1;
+    const unsigned last_off = (unsigned)(last_row / r_heads - t_seg) * (unsigned)a.h_q * 256u + (unsigned)(last_row % r_heads) * 256u;
+    int rt[2], rj[2];
+    unsigned swz[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = 8 * wave + 4 * i + (lane >> 4), full = row0 + r;
+      rt[i] = full / r_heads - t_seg;
+      rj[i] = full % r_heads;
+      swz[i] = (unsigned)((((lane & 15) ^ (r & 15))) << 4);
+    }
+    const int step_t = 32 / r_heads, step_j = 32 % r_heads;
+    auto request = [&](int slot) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        // rows past the last one repeat it: masked below
+        const unsigned off = min((unsigned)rt[i] * ((unsigned)a.h_q * 256u) + (unsigned)rj[i] * 256u, last_off);
+        lds_dma16_to(qb, off + swz[i], ring + slot * WT_TILE + (8 * wave + 4 * i) * 256);
+        rt[i] += step_t;
+        rj[i] += step_j;
+        if (rj[i] >= r_heads) rj[i] -= r_heads, ++rt[i];
+      }
+    };
+    const int n = seg_end - seg;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < n) request(i);
+    for (int i = 0; i < n; ++i) {
+      // tile i is there: two more may be under way. The statistics' loads were waited for by the compiler.
+      if (i + 2 < n) weigh_wait<4>();
+      else if (i + 1 < n) weigh_wait<2>();
+      else weigh_wait<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wavefront's statistics are written, its reads of tile i - 1 done
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (i + 3 < n) request((i + 3) & 3);
+      const unsigned char* const slot = smem + (i & 3) * WT_TILE;
+      pr_u32x4 qf[8];
+#pragma unroll
+      for (int st = 0; st < 8; ++st) qf[st] = *(const pr_u32x4*)(slot + q_addr[st]);
+      float4 ng[4];  // of rows 8 y + 4 g ..
+#pragma unroll
+      for (int y = 0; y < 4; ++y) ng[y] = *(const float4*)&neg[i * 32 + 8 * y + 4 * g];
+      f32x16 sc[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
+#pragma unroll
+        for (int st = 0; st < 8; ++st)
+          sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pr_bf16x8, qf[st]),
+                                                          __builtin_bit_cast(pr_bf16x8, k[b][st]), sc[b], 0, 0, 0);
+      }
+      const int tile_row = row0 + i * 32;
+      const bool whole = tile_row >= masked_below && tile_row + 32 <= rows && __builtin_amdgcn_readfirstlane(dead[i]) == 0;
+      if (whole) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float acc = 0.f;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 0], c2, ng[y].x));
+            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 1], c2, ng[y].y));
+            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 2], c2, ng[y].z));
+            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 3], c2, ng[y].w));
+          }
+          sum[b] += acc;
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float acc = 0.f;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float z = e == 0 ? ng[y].x : e == 1 ? ng[y].y : e == 2 ? ng[y].z : ng[y].w;
+              const int r = tile_row + 8 * y + 4 * g + e;
+              const bool seen = r >= first_row[b] && r < rows && z != -INFINITY;
+              const float p = __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + e], c2, z));
+              acc += seen ? p : 0.f;
+            }
+          sum[b] += acc;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const float w = sum_halves(sum[b]);
+    if (g != b || !here[b]) continue;
+    if (o.splits > 1) {
+      o.partial[(((size_t)split * a.n_seqs + s) * a.h_kv + h) * a.max_len + key0 + 32 * b + l32] = w;
+    } else {
+      float* const to = a.weight + at[b];
+      *to = o.accumulate ? *to + w : w;
+    }
+  }
+}
+
+// Adds the workgroups' shares in their order.
+constexpr int WA_THREADS = 256;
+__global__ __launch_bounds__(WA_THREADS) void weigh_add_kernel(PagedArgs a, WeighTiles o, int blocks) {
+  const int sh = blockIdx.x / blocks, s = sh / a.h_kv, h = sh - s * a.h_kv;
+  const long long key = (long long)(blockIdx.x - sh * blocks) * WA_THREADS + threadIdx.x;
+  if (key >= paged_seq_of(a, s).len) return;
+  const int page = a.table[(size_t)s * a.table_pages + ((int)key >> a.page_shift)];
+  if (!paged_page_ok(page, a.n_pages)) return;
+  float w = 0.f;
+  for (int i = 0; i < o.splits; ++i) w += o.partial[((size_t)i * a.n_seqs * a.h_kv + sh) * a.max_len + key];
+  float* const to = a.weight + paged_row(page, h, (int)key & ((1 << a.page_shift) - 1), a.h_kv, a.page_shift);
+  *to = o.accumulate ? *to + w : w;
+}
+
+// Rows above which a call takes the tiles (stacked rows of a KV head), and what their 32-bit arithmetic takes.
+constexpr long long WT_FROM_ROWS = 32, WT_MOST_ROWS = 1 << 26;
+constexpr int WT_MOST_HEADS = 1024;
+static bool weigh_tiled(const PagedArgs& a, int dtype, int d) {
+  const long long rows = (long long)a.max_new * (a.h_q / a.h_kv);
+  return dtype == QP_BF16 && d == 128 && rows > WT_FROM_ROWS && rows <= WT_MOST_ROWS && a.h_kv <= WT_MOST_HEADS;
+}
+// Workgroups that share a block of entries' rows: as many as make two per compute unit, of WT_MIN_TILES row tiles and more.
+static int weigh_splits(long long blocks, long long rows, size_t per_split, size_t scratch) {
+  const long long want = 2ll * device_cu_count() / std::max<long long>(blocks, 1);
+  const long long most = std::min<long long>(rows / (32 * WT_MIN_TILES), per_split > 0 ? (long long)(scratch / per_split) : 0);
+  return (int)std::max<long long>(1, std::min<long long>(std::min<long long>(want, most), 32));
+}
+static size_t weigh_per_split(int n_seqs, int h_kv, int max_len) { return (size_t)n_seqs * h_kv * max_len * sizeof(float); }
+static long long weigh_blocks(int n_seqs, int h_kv, int max_len) {
+  return ((long long)max_len + WT_KEYS - 1) / WT_KEYS * n_seqs * h_kv;
+}
+
+size_t paged_weigh_workspace_bytes(int n_seqs, int h_q, int h_kv, int max_new, int max_len) {
+  const long long rows = (long long)max_new * (h_q / h_kv);
+  const size_t per = weigh_per_split(n_seqs, h_kv, max_len);
+  const int splits = weigh_splits(weigh_blocks(n_seqs, h_kv, max_len), rows, per, ~(size_t)0);
+  return splits > 1 ? splits * per : 0;
+}
+
+template <bool F8>
+static bool weigh_tiles_as(const PagedArgs& a, const void* q, const float* lse, int accumulate, void* scratch, size_t scratch_bytes,
+                           hipStream_t s) {
+  const long long blocks = weigh_blocks(a.n_seqs, a.h_kv, a.max_len);
+  WeighTiles o{q, lse, accumulate, 1, (float*)scratch};
+  if (scratch != nullptr)
+    o.splits = weigh_splits(blocks, (long long)a.max_new * (a.h_q / a.h_kv), weigh_per_split(a.n_seqs, a.h_kv, a.max_len), scratch_bytes);
+  if (blocks * o.splits * WT_NW * 64 > PAGED_MAX_THREADS) return false;
+  hipLaunchKernelGGL((weigh_tile_kernel<F8>), dim3((unsigned)(blocks * o.splits)), dim3(WT_NW * 64), WT_LDS, s, a, o);
+  if (o.splits > 1) {
+    const int per = (a.max_len + WA_THREADS - 1) / WA_THREADS;
+    hipLaunchKernelGGL(weigh_add_kernel, dim3((unsigned)((long long)per * a.n_seqs * a.h_kv)), dim3(WA_THREADS), 0, s, a, o, per);
+  }
+  return true;
+}
 
 template <typename E, int D>
 static bool weigh_as(const PagedArgs& a, const void* q, const float* lse, int accumulate, hipStream_t s) {
@@ -108,8 +369,11 @@ static bool weigh_as(const PagedArgs& a, const void* q, const float* lse, int ac
   return true;
 }
 
-bool launch_paged_weigh(const PagedArgs& a, int dtype, int d, const void* q, const float* lse, int accumulate, void*, size_t,
-                        hipStream_t s) {
+bool launch_paged_weigh(const PagedArgs& a, int dtype, int d, const void* q, const float* lse, int accumulate, void* scratch,
+                        size_t scratch_bytes, hipStream_t s) {
+  if (weigh_tiled(a, dtype, d))
+    return a.fp8 ? weigh_tiles_as<true>(a, q, lse, accumulate, scratch, scratch_bytes, s)
+                 : weigh_tiles_as<false>(a, q, lse, accumulate, scratch, scratch_bytes, s);
   if (dtype == QP_F32) return d == 64 ? weigh_as<float, 64>(a, q, lse, accumulate, s) : weigh_as<float, 128>(a, q, lse, accumulate, s);
   if (a.fp8) return weigh_as<uint8_t, 128>(a, q, lse, accumulate, s);
   return d == 64 ? weigh_as<bf16_t, 64>(a, q, lse, accumulate, s) : weigh_as<bf16_t, 128>(a, q, lse, accumulate, s);

@@ -40,7 +40,7 @@ struct RowsBlock {
 
 // Two workgroups per compute unit where two blocks' rows fit half of the registers.
 template <typename E, int D, int RT>
-constexpr int pr_waves() { return D == 64 || (sizeof(E) < 4 && RT == 1) ? 2 : 1; }
+constexpr int pr_waves() { return D == 64 || (sizeof(E) < 4 && RT == 1) || sizeof(E) == 1 ? 2 : 1; }
 
 template <typename E, int D, int RT>
 __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
@@ -351,27 +351,29 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
   }
 }
 
-// Merge of the chunks' partial results of a row: out = sum_c 2^(lse_c - lse) O_c. One wavefront per row, up to 8 chunks' loads
-// under way together.
-constexpr int PM_WAVES = 4;
-template <typename T, int D>
-__global__ __launch_bounds__(PM_WAVES * 64) void paged_merge_kernel(PagedArgs a, PagedOut o) {
+// Merge of the chunks' partial results of a row: out = sum_c 2^(lse_c - lse) O_c. W wavefronts share a row, each with up to 8 chunks'
+// loads under way together; their results meet in LDS. One of 181 chunks per row alone took 42 us, a chain of 23 round trips.
+constexpr int PM_WAVES = 4;  // rows of a workgroup where a wavefront has a row to itself
+template <typename T, int D, int W>
+__global__ __launch_bounds__((W == 1 ? PM_WAVES : W) * 64) void paged_merge_kernel(PagedArgs a, PagedOut o) {
   constexpr int PER = D / 64;  // elements of a lane
+  constexpr int ROWS = W == 1 ? PM_WAVES : 1;
+  __shared__ float red[W][64][PER], red_m[W], red_l[W];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per_seq = (int)(((long long)a.max_new * a.h_q + PM_WAVES - 1) / PM_WAVES);
+  const int per_seq = (int)(((long long)a.max_new * a.h_q + ROWS - 1) / ROWS);
   const int s = blockIdx.x / per_seq;
   const PagedSeq q = paged_seq_of(a, s);
-  const long long item = (long long)(blockIdx.x - s * per_seq) * PM_WAVES + wave;
+  const long long item = (long long)(blockIdx.x - s * per_seq) * ROWS + (W == 1 ? wave : 0);
   const int i = (int)(item / a.h_q), qh = (int)(item - (long long)i * a.h_q);
-  if (i >= q.n) return;
+  if (i >= q.n) return;  // with W > 1: the whole workgroup
   const int n = q.len == 0 ? 1 : (q.len - 1) / o.chunk_keys + 1;  // chunks that answered
   const size_t total = (size_t)a.n_rows * a.h_q, at = (size_t)(q.row0 + i) * a.h_q + qh;
   constexpr int B = 8;
   float m = PR_NONE, den = 0.f, sum[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) sum[e] = 0.f;
-  for (int c0 = 0; c0 < n; c0 += B) {
+  for (int c0 = W == 1 ? 0 : wave * B; c0 < n; c0 += B * W) {
     float ls[B], po[B][PER];
 #pragma unroll
     for (int u = 0; u < B; ++u) {
@@ -401,12 +403,42 @@ __global__ __launch_bounds__(PM_WAVES * 64) void paged_merge_kernel(PagedArgs a,
     }
     m = mb;
   }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) red[wave][lane][e] = sum[e];
+    if (lane == 0) {
+      red_m[wave] = m;
+      red_l[wave] = den;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    m = red_m[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, red_m[w]);
+    den = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float wgt = __builtin_amdgcn_exp2f(red_m[w] - m);
+      den = fmaf(wgt, red_l[w], den);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) sum[e] = fmaf(wgt, red[w][lane][e], sum[e]);
+    }
+  }
   const bool none = den == 0.f;
   const float inv = none ? 0.f : 1.f / den;
 #pragma unroll
   for (int e = 0; e < PER; ++e) store_elem<T>((T*)o.out + at * D + PER * lane + e, none ? 0.f : sum[e] * inv);
   if (o.lse != nullptr && lane == 0)
     o.lse[(size_t)qh * a.n_rows + q.row0 + i] = none ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
+}
+// Eight wavefronts share a row of more than 16 chunks.
+constexpr int PM_SHARE = 8;
+static int merge_rows(int chunks) { return chunks > 16 ? 1 : PM_WAVES; }
+static long long merge_blocks(const PagedArgs& a, int chunks) {
+  const int rows = merge_rows(chunks);
+  return (((long long)a.max_new * a.h_q + rows - 1) / rows) * a.n_seqs;
 }
 
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes) {
@@ -426,7 +458,6 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   if (chunks > fit) {
     chunks = fit >= 2 ? fit : 1;
     keys = ((a.max_len + chunks - 1) / chunks + bk - 1) / bk * bk;
-    if (keys % (1 << a.page_shift) != 0 && chunks > 1) keys = (keys + 255) / 256 * 256;
     chunks = (a.max_len + keys - 1) / keys;
   }
   p.chunks = (int)std::max<long long>(chunks, 1);
@@ -442,8 +473,9 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
   if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1>), grid, block, 0, s, a, o);
   else hipLaunchKernelGGL((paged_rows_kernel<E, D, 2>), grid, block, 0, s, a, o);
   if (p.chunks > 1) {
-    const long long per_seq = ((long long)a.max_new * a.h_q + PM_WAVES - 1) / PM_WAVES;
-    hipLaunchKernelGGL((paged_merge_kernel<T, D>), dim3((unsigned)(per_seq * a.n_seqs)), dim3(PM_WAVES * 64), 0, s, a, o);
+    const dim3 merge((unsigned)merge_blocks(a, p.chunks));
+    if (merge_rows(p.chunks) == 1) hipLaunchKernelGGL((paged_merge_kernel<T, D, PM_SHARE>), merge, dim3(PM_SHARE * 64), 0, s, a, o);
+    else hipLaunchKernelGGL((paged_merge_kernel<T, D, 1>), merge, dim3(PM_WAVES * 64), 0, s, a, o);
   }
   return true;
 }
@@ -451,8 +483,7 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
 bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, void* out, float* lse, void* scratch,
                          size_t scratch_bytes, hipStream_t s) {
   const PagedPlan p = plan_paged_attend(a, dtype, d, scratch != nullptr ? scratch_bytes : 0);
-  const long long merge = (((long long)a.max_new * a.h_q + PM_WAVES - 1) / PM_WAVES) * a.n_seqs;
-  if (p.workgroups * PR_NW * 64 > PAGED_MAX_THREADS || merge * PM_WAVES * 64 > PAGED_MAX_THREADS) return false;
+  if (p.workgroups * PR_NW * 64 > PAGED_MAX_THREADS || merge_blocks(a, p.chunks) * PM_SHARE * 64 > PAGED_MAX_THREADS) return false;
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;

@@ -12,7 +12,7 @@
  *   qp_paged_evict    keeps the entries of most weight (and the first and the last ones), packed into other pages
  *
  * Conventions as in qp.h: data pointers are DEVICE pointers, tensors dense and row-major unless strides are given, 16-byte
- * aligned (4-byte ones for int32 / f32 arrays of one value per row or entry), the structs live in HOST memory, the library
+ * aligned (4-byte: int32 arrays and lse), the structs live in HOST memory, the library
  * allocates nothing, keeps no pointer and never waits for the GPU, all work is enqueued on `hip_stream` of the current
  * device, errors come back as qp_status and are found on the host before anything is launched. Same inputs (and the same
  * workspace size) give the same bits: nothing is summed by atomics.

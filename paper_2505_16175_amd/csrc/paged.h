@@ -85,9 +85,9 @@ struct PagedEvict {
   int to_pages;
   int32_t* to_len;
   int32_t* kept;      // [n_seqs][h_kv][keep], the caller's or in the workspace
-  uint32_t* keys;     // [n_seqs][h_kv][max_len] where the lengths do not fit LDS
+  uint32_t* keys;     // workspace of paged_evict_keys_bytes, nullptr where that is 0
 };
-size_t paged_evict_keys_bytes(int n_seqs, int h_kv, int max_len);  // 0 where the keys fit LDS
-bool launch_paged_evict(const PagedArgs& a, const PagedEvict& e, int elem_bytes_per_row, hipStream_t s);
+size_t paged_evict_keys_bytes(int n_seqs, int h_kv, int max_len);  // 0 where a workgroup holds a head's keys
+bool launch_paged_evict(const PagedArgs& a, const PagedEvict& e, int row_bytes, hipStream_t s);
 
 }  // namespace qp

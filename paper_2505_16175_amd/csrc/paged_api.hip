@@ -39,7 +39,7 @@ qp_status check(const qp_layout* L, const qp_paged_cache* c, const qp_paged_batc
   qp_status st = check_layout(L);
   if (st != QP_OK) return st;
   if (c == nullptr || b == nullptr) return QP_ERR_INVALID_ARG;
-  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->pos, 4) || (c->weight != nullptr && !aligned(c->weight, 4)))
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->pos, 4) || (c->weight != nullptr && !aligned(c->weight, 16)))
     return QP_ERR_INVALID_ARG;
   if (c->n_pages <= 0 || (c->format != QP_CACHE_SAME && c->format != QP_CACHE_FP8_E4M3)) return QP_ERR_INVALID_ARG;
   if (c->format == QP_CACHE_FP8_E4M3 && (L->dtype != QP_BF16 || L->head_dim != 128)) return QP_ERR_UNSUPPORTED;
@@ -152,7 +152,8 @@ qp_status qp_paged_evict(const qp_layout* L, const qp_paged_cache* cache, const 
   e.keep = keep, e.n_first = n_first, e.n_last = n_last;
   e.to_table = to_table, e.to_pages = to_pages, e.to_len = to_len;
   e.kept = kept_or_null != nullptr ? kept_or_null : (int32_t*)workspace;
-  e.keys = (uint32_t*)((unsigned char*)workspace + evict_kept_bytes(a.n_seqs, a.h_kv, keep));
+  if (qp::paged_evict_keys_bytes(a.n_seqs, a.h_kv, a.max_len) > 0)
+    e.keys = (uint32_t*)((unsigned char*)workspace + evict_kept_bytes(a.n_seqs, a.h_kv, keep));
   const int row_bytes = L->head_dim * (a.fp8 ? 1 : L->dtype == QP_F32 ? 4 : 2);
   return finish(qp::launch_paged_evict(a, e, row_bytes, (hipStream_t)hip_stream));
 }

@@ -2,13 +2,14 @@
 //
 // append   a copy: row r of head h -> its sequence's entry. Bound by HBM (2 rows in, 2 rows out per token and head) from a few
 //          thousand rows on, by the launch below.
-// evict    two launches. evict_select_kernel: one workgroup per (sequence, head) finds which entries stay, as order-preserving
-//          keys (an entry that stays in any case above all weights, one on a missing page out of the search) through
-//          select_threshold, and lists them in ascending order. evict_move_kernel: many workgroups copy the listed rows, which
-//          is where the bytes are (4 rows of head_dim per kept entry against 4 bytes per entry for the selection).
+// evict    two launches. evict_select_kernel: one workgroup per (sequence, head) finds the threshold among order-preserving keys
+//          (select_threshold) and lists the entries that stay, in order. evict_move_kernel: many workgroups copy the listed rows,
+//          which is where the bytes are (4 rows of head_dim per kept entry against 4 bytes per entry for the selection).
 #include "append.h"
 #include "paged.h"
 #include "select.h"
+
+#include <algorithm>
 
 namespace qp {
 
@@ -87,114 +88,186 @@ bool launch_paged_append(const PagedArgs& a, const PagedAppend& src, int dtype, 
 
 // ---- evict -----------------------------------------------------------------------------------------------------------
 
-constexpr int EV_LDS_KEYS = 32768;  // keys of longer sequences lie in the workspace
-constexpr int EV_LOADS = 8;         // entries per thread whose weights are under way together
+// Keys of a (sequence, head): 0 an entry on a missing page (or none), EV_STAYS one of the first or last, else the weight's order, kept
+// between the two. A thread takes four neighbours of a block of 4096: one page number and one load for the four.
 constexpr uint32_t EV_STAYS = 0xffffffffu;
+constexpr int EV_BLOCK = 4 * SEL_THREADS;
+constexpr int EV_HELD = 12;  // blocks whose keys the workgroup holds in registers; those of longer sequences lie in the workspace
 
 size_t paged_evict_keys_bytes(int n_seqs, int h_kv, int max_len) {
-  return max_len <= EV_LDS_KEYS ? 0 : (size_t)n_seqs * h_kv * max_len * sizeof(uint32_t);
+  const size_t blocks = ((size_t)max_len + EV_BLOCK - 1) / EV_BLOCK;
+  return blocks <= EV_HELD ? 0 : (size_t)n_seqs * h_kv * blocks * EV_BLOCK * sizeof(uint32_t);
 }
 
-// Keys: 0 an entry on a missing page, EV_STAYS one of the first or last, else the weight's order kept between the two.
-template <bool IN_LDS>
+// One workgroup has a head to itself, so an instruction per entry costs time: 46,125 of them 0.3 us. us for 16,384 kept of
+// 46,125 entries of 4 heads, one entry per thread and step, keys in the workspace 75, in LDS and registers 59; weights made into
+// dense keys by a launch of their own 6 and 25.
+template <bool HELD>
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, PagedEvict e) {
-  extern __shared__ uint32_t lds_keys[];
   __shared__ SelectLds lds;
-  __shared__ uint32_t wave_b[SEL_WAVES], wave_min[SEL_WAVES], wave_max[SEL_WAVES];
+  __shared__ uint32_t red[4][SEL_WAVES];
+  constexpr int RUNS = HELD ? EV_HELD : 1;  // blocks whose wavefronts' counts are there at a time
+  __shared__ __attribute__((aligned(16))) uint32_t run_gt[RUNS][SEL_WAVES], run_eq[RUNS][SEL_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int s = blockIdx.x / a.h_kv, h = blockIdx.x - s * a.h_kv;
+  const int sh = blockIdx.x, s = sh / a.h_kv, h = sh - s * a.h_kv;
   const int n = paged_len_of(a, s);
   const int mask = (1 << a.page_shift) - 1;
-  uint32_t* const keys = IN_LDS ? lds_keys : e.keys + ((size_t)s * a.h_kv + h) * a.max_len;
   const int32_t* const table = a.table + (size_t)s * a.table_pages;
+  const int used = (n + EV_BLOCK - 1) / EV_BLOCK;
+  uint32_t* const far = HELD ? nullptr : e.keys + (size_t)sh * (((size_t)a.max_len + EV_BLOCK - 1) / EV_BLOCK * EV_BLOCK);
 
-  uint32_t kmin = 0xffffffffu, kmax = 0u, present = 0;
-  for (int j0 = tid; j0 < n; j0 += EV_LOADS * SEL_THREADS) {
-    int page[EV_LOADS];
-    float w[EV_LOADS];
-#pragma unroll
-    for (int u = 0; u < EV_LOADS; ++u) page[u] = j0 + u * SEL_THREADS < n ? table[(j0 + u * SEL_THREADS) >> a.page_shift] : -1;
-#pragma unroll
-    for (int u = 0; u < EV_LOADS; ++u) {
-      const bool ok = paged_page_ok(page[u], a.n_pages);
-      w[u] = ok ? a.weight[paged_row(page[u], h, (j0 + u * SEL_THREADS) & mask, a.h_kv, a.page_shift)] : 0.f;
+  uint32_t v[4] = {0xffffffffu, 0u, 0u, 0u};  // smallest and largest key of those that compete, entries present, entries that stay
+  auto load_page = [&](int u) { return u * EV_BLOCK + 4 * tid < n ? table[(u * EV_BLOCK + 4 * tid) >> a.page_shift] : -1; };
+  auto load_weights = [&](int u, int page) {
+    const int j = u * EV_BLOCK + 4 * tid;
+    return paged_page_ok(page, a.n_pages) ? *(const float4*)(a.weight + paged_row(page, h, j & mask, a.h_kv, a.page_shift))
+                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  auto key_of = [&](float w, int j, bool here) {
+    if (!here || j >= n) return 0u;
+    ++v[2];
+    if (j < e.n_first || j >= n - e.n_last) {
+      ++v[3];
+      return EV_STAYS;
     }
+    const uint32_t key = min(max(order_key(w), 1u), EV_STAYS - 1);
+    v[0] = min(v[0], key);
+    v[1] = max(v[1], key);
+    return key;
+  };
+  auto keys_of = [&](int u, int page, const float4& w) {
+    const int j = u * EV_BLOCK + 4 * tid;
+    const bool here = paged_page_ok(page, a.n_pages);
+    return make_uint4(key_of(w.x, j, here), key_of(w.y, j + 1, here), key_of(w.z, j + 2, here), key_of(w.w, j + 3, here));
+  };
+  uint4 held[HELD ? EV_HELD : 1];
+  if constexpr (HELD) {
+    int page[EV_HELD];
 #pragma unroll
-    for (int u = 0; u < EV_LOADS; ++u) {
-      const int j = j0 + u * SEL_THREADS;
-      if (j >= n) continue;
-      uint32_t key = 0;
-      if (paged_page_ok(page[u], a.n_pages)) {
-        key = j < e.n_first || j >= n - e.n_last ? EV_STAYS : min(max(order_key(w[u]), 1u), EV_STAYS - 1);
-        kmin = min(kmin, key);
-        kmax = max(kmax, key);
-        ++present;
-      }
-      keys[j] = key;
+    for (int u = 0; u < EV_HELD; ++u) page[u] = load_page(u);
+#pragma unroll
+    for (int u0 = 0; u0 < EV_HELD; u0 += 6) {
+      float4 w[6];
+#pragma unroll
+      for (int u = 0; u < 6; ++u) w[u] = load_weights(u0 + u, page[u0 + u]);
+#pragma unroll
+      for (int u = 0; u < 6; ++u) held[u0 + u] = keys_of(u0 + u, page[u0 + u], w[u]);
+      __builtin_amdgcn_sched_barrier(0);  // or the second half's loads come first and push keys out of the registers
+    }
+  } else {
+    for (int u0 = 0; u0 < used; u0 += 4) {
+      int page[4];
+      float4 w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) page[u] = load_page(u0 + u);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w[u] = load_weights(u0 + u, page[u]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (u0 + u < used) *(uint4*)(far + (size_t)(u0 + u) * EV_BLOCK + 4 * tid) = keys_of(u0 + u, page[u], w[u]);
     }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
-    kmin = min(kmin, (uint32_t)__shfl_xor((int)kmin, o, 64));
-    kmax = max(kmax, (uint32_t)__shfl_xor((int)kmax, o, 64));
-    present += (uint32_t)__shfl_xor((int)present, o, 64);
+    v[0] = min(v[0], (uint32_t)__shfl_xor((int)v[0], o, 64));
+    v[1] = max(v[1], (uint32_t)__shfl_xor((int)v[1], o, 64));
+    v[2] += (uint32_t)__shfl_xor((int)v[2], o, 64);
+    v[3] += (uint32_t)__shfl_xor((int)v[3], o, 64);
   }
-  if (lane == 0) {
-    wave_min[wave] = kmin;
-    wave_max[wave] = kmax;
-    wave_b[wave] = present;
-  }
+  if (lane == 0) red[0][wave] = v[0], red[1][wave] = v[1], red[2][wave] = v[2], red[3][wave] = v[3];
   lds.hist[2 * tid] = 0;
   lds.hist[2 * tid + 1] = 0;
   if (tid == 0) lds.list_n = 0;
-  __syncthreads();  // also orders the keys in the workspace: one workgroup wrote them and reads them
-  uint32_t lo = 0xffffffffu, hi = 0u, total = 0;
+  __syncthreads();  // every thread reads the keys in the workspace that it wrote itself
+  uint32_t lo = 0xffffffffu, hi = 0u, total = 0, stays = 0;
 #pragma unroll
   for (int w = 0; w < SEL_WAVES; ++w) {
-    lo = min(lo, wave_min[w]);
-    hi = max(hi, wave_max[w]);
-    total += wave_b[w];
+    lo = min(lo, red[0][w]);
+    hi = max(hi, red[1][w]);
+    total += red[2][w];
+    stays += red[3][w];
   }
+  auto key4 = [&](int u) { return u < used ? *(const uint4*)(far + (size_t)u * EV_BLOCK + 4 * tid) : make_uint4(0u, 0u, 0u, 0u); };
+  auto each = [&](auto f) {
+    if constexpr (HELD) {
+#pragma unroll
+      for (int u = 0; u < EV_HELD; ++u)
+        if (u < used) f(held[u].x, true), f(held[u].y, true), f(held[u].z, true), f(held[u].w, true);
+    } else {
+      for (int u0 = 0; u0 < used; u0 += 8) {
+        uint4 k[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) k[u] = key4(u0 + u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) f(k[u].x, true), f(k[u].y, true), f(k[u].z, true), f(k[u].w, true);
+      }
+    }
+  };
   const uint32_t count = min(total, (uint32_t)e.keep);
   uint32_t thr = 0, need = 0;  // every present entry stays
-  if (count < total) select_threshold([&](int j) { return keys[j]; }, n, lo, hi, count, lds, thr, need);
+  if (count < total) {
+    thr = EV_STAYS - 1;        // only those that stay in any case
+    if (count > stays)         // and the largest of the others, whose keys alone the search spreads over its buckets
+      select_threshold<false>(each, lo, hi, count - stays, lds, thr, need);
+  }
 
-  // list: wavefront w owns a run of entries and walks it 64 at a time
-  const int run = ((n + SEL_WAVES - 1) / SEL_WAVES + 63) / 64 * 64;
-  const int j_begin = min(wave * run, n), j_end = min(j_begin + run, n);
-  uint32_t gt = 0, eq = 0;
-  for (int j0 = j_begin; j0 < j_end; j0 += 64) {
-    const bool in = j0 + lane < j_end;
-    const uint32_t key = in ? keys[j0 + lane] : 0u;
-    gt += (uint32_t)__popcll(__ballot(in && key > thr));
-    eq += (uint32_t)__popcll(__ballot(in && key == thr));
-  }
-  __syncthreads();  // wave_min / wave_max have been read
-  if (lane == 0) {
-    wave_min[wave] = gt;
-    wave_max[wave] = eq;
-  }
-  __syncthreads();
-  uint32_t gt_before = 0, eq_run = 0;
-#pragma unroll
-  for (int w = 0; w < SEL_WAVES; ++w) {
-    gt_before += w < wave ? wave_min[w] : 0u;
-    eq_run += w < wave ? wave_max[w] : 0u;
-  }
-  uint32_t slot0 = gt_before + min(eq_run, need);
-  int32_t* const kept = e.kept + ((size_t)s * a.h_kv + h) * e.keep;
+  // The list, in order: an entry above the threshold stays, one equal to it if fewer than `need` of those lie before it, and its
+  // slot is the number of survivors before it, gt + min(eq, need) of the keys above and equal there.
+  int32_t* const kept = e.kept + (size_t)sh * e.keep;
   const unsigned long long below = (1ull << lane) - 1ull;
-  for (int j0 = j_begin; j0 < j_end; j0 += 64) {
-    const bool in = j0 + lane < j_end;
-    const uint32_t key = in ? keys[j0 + lane] : 0u;
-    const bool is_eq = in && key == thr;
-    const unsigned long long be = __ballot(is_eq);
-    const bool keep_it = (in && key > thr) || (is_eq && eq_run + (uint32_t)__popcll(be & below) < need);
-    const unsigned long long bs = __ballot(keep_it);
-    const uint32_t slot = slot0 + (uint32_t)__popcll(bs & below);
-    if (keep_it && slot < (uint32_t)e.keep) kept[slot] = j0 + lane;
-    slot0 += (uint32_t)__popcll(bs);
-    eq_run += (uint32_t)__popcll(be);
+  auto tally = [&](const uint4& k, int r) {
+    const uint32_t x = (uint32_t)(__popcll(__ballot(k.x > thr)) + __popcll(__ballot(k.y > thr)) + __popcll(__ballot(k.z > thr)) + __popcll(__ballot(k.w > thr)));
+    const uint32_t y = (uint32_t)(__popcll(__ballot(k.x == thr)) + __popcll(__ballot(k.y == thr)) + __popcll(__ballot(k.z == thr)) + __popcll(__ballot(k.w == thr)));
+    if (lane == 0) run_gt[r][wave] = x, run_eq[r][wave] = y;
+  };
+  auto emit = [&](const uint4& k, int j, uint32_t gt, uint32_t eq) {  // gt, eq: before this wavefront's run
+    const uint32_t key[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      gt += (uint32_t)__popcll(__ballot(key[c] > thr) & below);
+      eq += (uint32_t)__popcll(__ballot(key[c] == thr) & below);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint32_t slot = gt + min(eq, need);
+      if ((key[c] > thr || (key[c] == thr && eq < need)) && slot < (uint32_t)e.keep) kept[slot] = j + c;
+      gt += key[c] > thr;
+      eq += key[c] == thr;
+    }
+  };
+  // the comparisons are cheaper to make again than to keep
+  auto forget = [](uint4& k) { asm volatile("" : "+v"(k.x), "+v"(k.y), "+v"(k.z), "+v"(k.w)); };
+  uint32_t gt = 0, eq = 0;  // before the block
+  auto block = [&](const uint4& k, int u, int r) {
+    uint32_t gt_w = gt, eq_w = eq;
+#pragma unroll
+    for (int w = 0; w < SEL_WAVES; w += 4) {
+      const uint4 x = *(const uint4*)&run_gt[r][w], y = *(const uint4*)&run_eq[r][w];
+      gt_w += (w < wave ? x.x : 0u) + (w + 1 < wave ? x.y : 0u) + (w + 2 < wave ? x.z : 0u) + (w + 3 < wave ? x.w : 0u);
+      eq_w += (w < wave ? y.x : 0u) + (w + 1 < wave ? y.y : 0u) + (w + 2 < wave ? y.z : 0u) + (w + 3 < wave ? y.w : 0u);
+      gt += x.x + x.y + x.z + x.w;
+      eq += y.x + y.y + y.z + y.w;
+    }
+    emit(k, u * EV_BLOCK + 4 * tid, gt_w, eq_w);
+  };
+  if constexpr (HELD) {
+#pragma unroll
+    for (int u = 0; u < EV_HELD; ++u)
+      if (u < used) tally(held[u], u);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < EV_HELD; ++u) {
+      forget(held[u]);
+      if (u < used) block(held[u], u, u);
+    }
+  } else {
+    for (int u = 0; u < used; ++u) {
+      const uint4 k = key4(u);
+      __syncthreads();  // the counts of the block before have been read
+      tally(k, 0);
+      __syncthreads();
+      block(k, u, 0);
+    }
   }
   for (uint32_t x = count + tid; x < (uint32_t)e.keep; x += SEL_THREADS) kept[x] = -1;
   if (h == 0 && tid == 0) e.to_len[s] = (int)count;
@@ -252,31 +325,20 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move_kernel(PagedArgs a, Pag
 }
 
 template <int LPR>
-static bool move_as(const PagedArgs& a, const PagedEvict& e, hipStream_t s) {
+static bool evict_as(const PagedArgs& a, const PagedEvict& e, hipStream_t s) {
   constexpr int ROWS = EM_THREADS / LPR * EM_UNROLL;
   const long long per = ((long long)e.keep + ROWS - 1) / ROWS;
   const long long heads = (long long)a.n_seqs * a.h_kv;
   if (per * heads * EM_THREADS > PAGED_MAX_THREADS || heads * SEL_THREADS > PAGED_MAX_THREADS) return false;
-  const bool in_lds = a.max_len <= EV_LDS_KEYS;
-  if (in_lds) {
-    static bool attr_set[QP_MAX_DEVICES] = {};
-    const int dev = current_device();
-    if (dev < 0 || !attr_set[dev]) {
-      (void)hipFuncSetAttribute((const void*)evict_select_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                EV_LDS_KEYS * (int)sizeof(uint32_t));
-      if (dev >= 0) attr_set[dev] = true;
-    }
-    hipLaunchKernelGGL(evict_select_kernel<true>, dim3((unsigned)heads), dim3(SEL_THREADS), (size_t)a.max_len * sizeof(uint32_t), s,
-                       a, e);
-  } else {
-    hipLaunchKernelGGL(evict_select_kernel<false>, dim3((unsigned)heads), dim3(SEL_THREADS), 0, s, a, e);
-  }
+  const dim3 grid((unsigned)heads), block(SEL_THREADS);
+  if (e.keys == nullptr) hipLaunchKernelGGL(evict_select_kernel<true>, grid, block, 0, s, a, e);
+  else hipLaunchKernelGGL(evict_select_kernel<false>, grid, block, 0, s, a, e);
   hipLaunchKernelGGL(evict_move_kernel<LPR>, dim3((unsigned)(per * heads)), dim3(EM_THREADS), 0, s, a, e, (int)per);
   return true;
 }
 
 bool launch_paged_evict(const PagedArgs& a, const PagedEvict& e, int row_bytes, hipStream_t s) {
-  return row_bytes == 128 ? move_as<8>(a, e, s) : row_bytes == 256 ? move_as<16>(a, e, s) : move_as<32>(a, e, s);
+  return row_bytes == 128 ? evict_as<8>(a, e, s) : row_bytes == 256 ? evict_as<16>(a, e, s) : evict_as<32>(a, e, s);
 }
 
 }  // namespace qp

@@ -18,7 +18,7 @@ constexpr int SEL_WAVES = SEL_THREADS / 64;
 constexpr int SEL_BITS = 11;
 constexpr int SEL_NB = 1 << SEL_BITS;  // buckets per round, two per thread
 constexpr int SEL_LIST = 256;          // a bucket of at most this many keys is ranked directly
-constexpr int SEL_UNROLL = 2;          // independent key reads per thread and loop trip
+constexpr int SEL_UNROLL = 2;          // independent reads of keys in LDS per thread and loop trip
 constexpr int SEL_MAX_ROUNDS = 4;      // 3 suffice for 32-bit keys; the bound makes termination explicit
 static_assert(SEL_NB == 2 * SEL_THREADS, "two buckets per thread");
 
@@ -29,50 +29,65 @@ __device__ __forceinline__ uint32_t order_key(float s) {
 }
 
 struct SelectLds {
-  __attribute__((aligned(8))) uint32_t hist[SEL_NB];  // zero at entry, and again when the search returns
+  __attribute__((aligned(16))) uint32_t hist[SEL_NB];  // zero at entry, and again when the search returns
   uint32_t list[SEL_LIST];
   uint32_t wave_a[SEL_WAVES];
   uint32_t sel_bucket, sel_need, sel_count, sel_key, list_n;  // list_n: zero at entry
 };
 
-// thr: the rank-th largest of the keys key_at(0) .. key_at(n - 1) inside [lo, hi] (1 <= rank <= their number; keys outside do
-// not take part); need: how many keys equal to it are among the first `rank` (>= 1). The workgroup has met at a barrier behind
-// what it wrote to `lds` and to the keys.
-template <class KeyAt>
-__device__ __forceinline__ void select_threshold(KeyAt key_at, int n, uint32_t lo, uint32_t hi, uint32_t rank, SelectLds& lds,
+// Every key of key_at(0) .. key_at(n - 1) once, by whole wavefronts: f(key, whether there is one).
+template <int UNROLL, class KeyAt>
+struct EachKey {
+  KeyAt key_at;
+  int n;
+  template <class F>
+  __device__ __forceinline__ void operator()(F f) const {
+    const int n_round = (n + SEL_THREADS - 1) / SEL_THREADS * SEL_THREADS;  // whole wavefronts take part
+    for (int j0 = threadIdx.x; j0 < n_round; j0 += UNROLL * SEL_THREADS) {
+      uint32_t kk[UNROLL];
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) kk[u] = j0 + u * SEL_THREADS < n ? key_at(j0 + u * SEL_THREADS) : 0u;
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) f(kk[u], j0 + u * SEL_THREADS < n);  // beyond n_round no lane has one
+    }
+  }
+};
+template <int UNROLL = SEL_UNROLL, class KeyAt>
+__device__ __forceinline__ EachKey<UNROLL, KeyAt> each_key(KeyAt key_at, int n) {
+  return EachKey<UNROLL, KeyAt>{key_at, n};
+}
+
+// thr: the rank-th largest of the keys that `each` hands to the workgroup's threads, as far as they are inside [lo, hi]
+// (1 <= rank <= their number); need: how many keys equal to it are among the first `rank` (>= 1). The workgroup has met at a
+// barrier behind what it wrote to `lds` and to the keys. FOLD: keys that share a bucket are counted together first (above); without
+// it a list of equal keys takes a few times longer and every other one less.
+template <bool FOLD = true, class Each>
+__device__ __forceinline__ void select_threshold(Each each, uint32_t lo, uint32_t hi, uint32_t rank, SelectLds& lds,
                                                  uint32_t& thr, uint32_t& need) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n_round = (n + SEL_THREADS - 1) / SEL_THREADS * SEL_THREADS;  // whole wavefronts take part
   uint32_t span = hi - lo;          // keys still in play: lo <= key <= lo + span
   need = rank;                      // of T among them, counted from the largest
   thr = lo;
   for (int round = 0; round < SEL_MAX_ROUNDS; ++round) {
     const int bits = span ? 32 - __builtin_clz(span) : 0;
     const int sh = bits > SEL_BITS ? bits - SEL_BITS : 0;
-    for (int j0 = tid; j0 < n_round; j0 += SEL_UNROLL * SEL_THREADS) {
-      uint32_t kk[SEL_UNROLL];
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) kk[u] = j0 + u * SEL_THREADS < n ? key_at(j0 + u * SEL_THREADS) : 0u;
-#pragma unroll
-      for (int u = 0; u < SEL_UNROLL; ++u) {
-        const int j = j0 + u * SEL_THREADS;  // j >= n_round only when j >= n: such a batch has no active lane
-        const uint32_t off = kk[u] - lo;
-        bool act = j < n && off <= span;  // a key below lo wraps to a large offset
-        const uint32_t bin = off >> sh;
-        const unsigned long long am = __ballot(act);
-        if (am != 0) {  // fold the first active lane's bucket when many lanes share it
-          const int leader = __ffsll((long long)am) - 1;
-          const uint32_t b0 = (uint32_t)__builtin_amdgcn_readlane((int)bin, leader);
-          const bool mine = act && bin == b0;
-          const unsigned long long same = __ballot(mine);
-          if (__popcll(same) >= 8) {
-            if (lane == leader) atomicAdd(&lds.hist[b0], (uint32_t)__popcll(same));
-            if (mine) act = false;
-          }
+    each([&](uint32_t key, bool in) {
+      const uint32_t off = key - lo;
+      bool act = in && off <= span;  // a key below lo wraps to a large offset
+      const uint32_t bin = off >> sh;
+      const unsigned long long am = __ballot(act);
+      if (FOLD && am != 0) {  // fold the first active lane's bucket when many lanes share it
+        const int leader = __ffsll((long long)am) - 1;
+        const uint32_t b0 = (uint32_t)__builtin_amdgcn_readlane((int)bin, leader);
+        const bool mine = act && bin == b0;
+        const unsigned long long same = __ballot(mine);
+        if (__popcll(same) >= 8) {
+          if (lane == leader) atomicAdd(&lds.hist[b0], (uint32_t)__popcll(same));
+          if (mine) act = false;
         }
-        if (act) atomicAdd(&lds.hist[bin], 1u);
       }
-    }
+      if (act) atomicAdd(&lds.hist[bin], 1u);
+    });
     __syncthreads();
     // suffix sums over the buckets: this thread owns buckets 2 tid and 2 tid + 1 (and clears them for a next round)
     const uint2 hb = *(const uint2*)&lds.hist[2 * tid];
@@ -109,18 +124,23 @@ __device__ __forceinline__ void select_threshold(KeyAt key_at, int n, uint32_t l
     if (sh == 0) break;  // buckets were single keys: T = lo, `need` of its copies survive
     if (count <= SEL_LIST) {
       // rank the bucket's keys directly
-      for (int j = tid; j < n; j += SEL_THREADS) {
-        const uint32_t key = key_at(j);
-        if (key - lo <= span) {
+      each([&](uint32_t key, bool in) {
+        if (in && key - lo <= span) {
           const uint32_t p = atomicAdd(&lds.list_n, 1u);
           if (p < (uint32_t)SEL_LIST) lds.list[p] = key;  // always true: the bucket holds `count` keys
         }
-      }
+      });
       __syncthreads();
       if (tid < (int)count) {
         const uint32_t x = lds.list[tid];
         uint32_t g = 0, e = 0;
-        for (uint32_t m = 0; m < count; ++m) {
+        uint32_t m = 0;
+        for (; m + 4 <= count; m += 4) {
+          const uint4 y = *(const uint4*)&lds.list[m];
+          g += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+          e += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
+        }
+        for (; m < count; ++m) {
           const uint32_t y = lds.list[m];
           g += y > x;
           e += y == x;

@@ -116,7 +116,7 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
   }
 
   uint32_t thr, need;
-  select_threshold([&](int j) { return keys[j]; }, n, lo, hi, (uint32_t)a.keep, lds, thr, need);
+  select_threshold(each_key([&](int j) { return keys[j]; }, n), lo, hi, (uint32_t)a.keep, lds, thr, need);
   // thr: the k-th largest key; need: how many keys equal to it survive (>= 1)
 
   // this workgroup's slice of the tokens, and the (greater, equal) keys before it

@@ -365,7 +365,8 @@ def test_append_without_weights_and_refusals_of_the_binding():
     (L7, 64, False, [700, 300, 65], 200, 4, 16, []), (L7, 16, False, [1, 0, 17], 8, 1, 1, []), (TINY, 32, False, [100, 64], 64, 0, 0, [(0, 1), (1, 0)]),
     (F32, 16, False, [77], 33, 33, 0, []), (BF64, 128, False, [900, 128], 129, 0, 129, []), (L72, 32, True, [513, 100], 99, 3, 50, [(0, 7)]),
     (ODD, 16, False, [48, 47], 1, 0, 0, []), (ODD, 256, True, [1000], 1000, 4, 4, []), (TINY, 16, False, [9000], 4500, 4, 64, []),
-    (L7, 64, False, [40000, 33000], 9999, 4, 64, [(0, 100)]), (TINY, 64, False, [33], 40, 20, 20, []), (TINY, 16, False, [32, 16], 10, 5, 5, [(0, 0), (0, 1), (1, 0)])])
+    (L7, 64, False, [40000, 33000, 36865], 9999, 4, 64, [(0, 100), (0, 600)]), (L7, 128, False, [49152, 36864], 30000, 0, 12000, []),
+    (TINY, 256, False, [60000, 100], 20000, 4, 64, [(0, 200)]), (TINY, 64, False, [33], 40, 20, 20, []), (TINY, 16, False, [32, 16], 10, 5, 5, [(0, 0), (0, 1), (1, 0)])])
 @pytest.mark.parametrize("weights", ["spread", "ties"])
 def test_evict(layout, page, fp8, lens, keep, first, last, missing, weights):
     pages = -(-keep // page)

@@ -57,11 +57,13 @@
 //   * Workgroup ids are mapped so that the workgroups of one KV head run on the same XCDs (ids are
 //     dealt round-robin over the 8 XCDs, each with its own L2): with 4 KV heads, XCDs 2h and 2h+1
 //     serve head h, so every L2 streams one head's K/V instead of all of them.
+#include "paged_rows.h"
 #include "qp_internal.h"
 
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace qp {
 
@@ -150,17 +152,178 @@ __device__ __forceinline__ u32x4 widen8(uint2 p) {
 struct true_type { static constexpr bool value = true; };
 struct false_type { static constexpr bool value = false; };
 
+// A batch's chunks over the paged cache. Of the AttendArgs: q, out, lse, h_q, h_kv, scale_log2, the pools in ck and cv, n_split key
+// chunks of split_tiles tiles, part_o and part_lse [chunk][row][H_q] as paged_merge_kernel reads them; n_g is filled per workgroup.
+struct PagedTileArgs : AttendArgs {
+  PagedArgs pg;
+  int row_blocks;  // of 256 stacked rows, for max_new tokens
+  int chunk;       // filled per workgroup
+};
+__device__ unsigned char paged_zeros[8 * 256];  // eight rows of a missing page
+
+// A wavefront's 32 rows of a chunk (or of the whole): partial results, or the output. Where a result is not finite, a value that
+// some of its rows do not see may have reached them (0 times infinity): such rows are done again, 16 at a time, by the arithmetic
+// for few rows, which keeps those apart.
+template <bool F8>
+__device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const PagedSeq& seq, int seq_no, int h, int chunk, unsigned char* smem,
+                                             int wave, bool wave_live, int row0, int n_rows, int key_begin, int key_end, float m_run,
+                                             float l_run, f32x16 (&o)[4]) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int r_heads = a.h_q / a.h_kv;
+  const size_t total = (size_t)a.pg.n_rows * a.h_q;
+  const bool split = a.n_split > 1;
+  const bool staged = split && n_rows > MF_HB;
+  if (staged) __syncthreads();  // the ring's last readers
+  if (!wave_live) return;
+  // output row of stacked row r of the head: row0 + r is token t, query head j
+  const int t0 = row0 / r_heads, j0 = row0 - t0 * r_heads;
+  const float inv_r = 1.f / (float)r_heads;
+  auto place = [&](int r, size_t& at, size_t& lse_at) {
+    const int x = j0 + r, t = (int)(((float)x + 0.5f) * inv_r);  // x < 32 + R: exact
+    const int qh = h * r_heads + x - t * r_heads;
+    at = (size_t)(seq.row0 + t0 + t) * a.h_q + qh;
+    lse_at = (size_t)qh * a.pg.n_rows + seq.row0 + t0 + t;
+  };
+  const float l_tot = sum_halves(l_run);
+  bool bad = false;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad = bad || pr_not_finite(o[n][r]);
+  if (__any(bad)) {
+    using E = std::conditional_t<F8, uint8_t, bf16_t>;
+    for (int half = 0; half < 32 && row0 + half < n_rows; half += 16) {
+      RowsWave<E, MF_D, 1> rows;
+      const int count = min(16, n_rows - row0 - half);
+      rows.init(a.pg, seq, a.q, h, row0 + half, count);
+      const int end = min(key_end, min(seq.len, seq.base + (row0 + half + count - 1) / r_heads + 1));
+      for (int key = key_begin; key < end; key += RowsLayout<E, MF_D>::BK) {
+        RowsBlock<E, MF_D> b;
+        rows.load(b, a.pg, h, key, end, [&](int k) {
+          return __builtin_amdgcn_readfirstlane(a.pg.table[(size_t)seq_no * a.pg.table_pages + (k >> a.pg.page_shift)]);
+        });
+        rows.compute(b, key, end, a.scale_log2);
+      }
+      const float den = rows.denominator(0);
+      const bool none = den == 0.f;
+      const float inv = none ? 0.f : 1.f / den, lse2 = none ? -INFINITY : rows.m[0] + log2f(den);
+      if (rows.l16 >= count) continue;
+      size_t at, lse_at;
+      place(half + rows.l16, at, lse_at);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = none ? 0.f : rows.acc[0][e][r] * inv;
+          const int d = 32 * rows.g + 8 * r + e;
+          if (split) a.part_o[((size_t)chunk * total + at) * MF_D + d] = x;
+          else ((bf16_t*)a.out)[at * MF_D + d] = f32_to_bf16_rne(x);
+        }
+      if (rows.g == 0) {
+        if (split) a.part_lse[(size_t)chunk * total + at] = lse2;
+        else if (a.lse != nullptr) a.lse[lse_at] = lse2 * 0.6931471805599453f;
+      }
+    }
+    return;
+  }
+  const bool row_ok = row0 + l32 < n_rows, none = l_tot == 0.f;
+  const float inv = none ? 0.f : 1.f / l_tot;
+  const float lse2 = none ? -INFINITY : m_run * a.scale_log2 + log2f(l_tot);
+  size_t at, lse_at;
+  place(l32, at, lse_at);
+  if (split && row_ok && g == 0) a.part_lse[(size_t)chunk * total + at] = lse2;
+  if (staged) {
+    // through LDS as below: a store then writes two whole rows
+    const int rot = (blockIdx.x >> 3) * 5 + (blockIdx.x & 7) * 2 + wave;
+    unsigned char* const stage = smem + wave * (32 * MF_D * 4);
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *(float4*)(stage + l32 * (MF_D * 4) + ((8 * n + 2 * q4 + g) ^ (l32 & 15)) * 16) =
+            make_float4(o[n][4 * q4] * inv, o[n][4 * q4 + 1] * inv, o[n][4 * q4 + 2] * inv, o[n][4 * q4 + 3] * inv);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wavefront's writes before its reads
+#pragma unroll 4
+    for (int u = 0; u < 16; ++u) {
+      const int r = 2 * ((u + rot) & 15) + g;
+      size_t to, unused;
+      place(r, to, unused);
+      if (row0 + r < n_rows)
+        *(float4*)(a.part_o + ((size_t)chunk * total + to) * MF_D + 4 * l32) = *(const float4*)(stage + r * (MF_D * 4) + (l32 ^ (r & 15)) * 16);
+    }
+    return;
+  }
+  if (!row_ok) return;
+  if (split) {
+    float* const po = a.part_o + ((size_t)chunk * total + at) * MF_D;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *(float4*)(po + 32 * n + 8 * q4 + 4 * g) =
+            make_float4(o[n][4 * q4] * inv, o[n][4 * q4 + 1] * inv, o[n][4 * q4 + 2] * inv, o[n][4 * q4 + 3] * inv);
+    return;
+  }
+  bf16_t* const orow = (bf16_t*)a.out + at * MF_D;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      bf16x4 pk;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[e] = (__bf16)(o[n][4 * q4 + e] * inv);
+      *(uint2*)(orow + 32 * n + 8 * q4 + 4 * g) = __builtin_bit_cast(uint2, pk);
+    }
+  if (a.lse != nullptr && g == 0) a.lse[lse_at] = lse2 * 0.6931471805599453f;
+}
+
 // F8: the cache's K~ and V~ hold one E4M3 byte per element (the pruned cache's 8-bit format). Their tiles cannot go
 // global -> LDS directly: every wavefront loads its share of a tile into registers one tile ahead (8 bytes per lane
 // and row), widens it exactly to bf16 and writes it to the ring slot in the same swizzled layout, so that everything
 // after the staging is the same code. The group's own tiles are bf16 and staged as usual.
-template <bool F8>
-__global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
+//
+// Args = PagedTileArgs: a chunk of new tokens of each sequence of a batch over its pages (qp_paged.h). One segment: the new
+// tokens are the last entries, so row t sees the entries up to base + t. A wavefront's eight keys of a tile lie in one page, whose
+// number it reads from a register that holds the next 64 of the table; eight keys of a missing page are read from zeros and masked.
+// Denominators are summed in f32 from the unrounded numerators, since lse is an f32 result here.
+template <bool F8, class Args>
+__global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
+  constexpr bool PAGED = std::is_same_v<Args, PagedTileArgs>;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // wave-uniform for the compiler too: scalar address and branch work
   const int l32 = lane & 31, g = lane >> 5;
   const int r_heads = a.h_q / a.h_kv;
+  PagedSeq seq{};  // PAGED: this workgroup's sequence
+  int h, item, seq_no = 0;
+  if constexpr (PAGED) {
+    // workgroup id -> (KV head, sequence, key chunk, row block): all row blocks of a chunk on one XCD, whose L2 fetches its keys once
+    const int wg = blockIdx.x, xcd = wg & 7, idx = wg >> 3;
+    int unit;
+    if (8 % a.h_kv == 0) {
+      const int per = 8 / a.h_kv;
+      h = xcd / per;
+      unit = idx / a.row_blocks * per + xcd % per;
+      item = idx % a.row_blocks;
+    } else if (a.h_kv % 8 == 0) {
+      const int hp = a.h_kv / 8, rest = idx / hp;
+      h = (idx % hp) * 8 + xcd;
+      unit = rest / a.row_blocks;
+      item = rest % a.row_blocks;
+    } else {
+      const int rest = wg / a.h_kv;
+      h = wg % a.h_kv;
+      unit = rest / a.row_blocks;
+      item = rest % a.row_blocks;
+    }
+    seq_no = unit % a.pg.n_seqs;
+    a.chunk = unit / a.pg.n_seqs;
+    if (a.chunk >= a.n_split) return;
+    seq = paged_seq_of(a.pg, seq_no);
+    a.n_g = seq.n;
+    if (a.chunk > 0 && a.chunk * a.split_tiles >= (seq.len + MF_BN - 1) / MF_BN) return;  // chunk 0 always answers
+  }
+  const int base = PAGED ? seq.base : 0;  // PAGED: entries before the new tokens
   int n_rows = a.n_g * r_heads;
   int n_hb = (n_rows + MF_HB - 1) / MF_HB;  // half blocks of 128 rows
   int n_rb = (n_hb + 1) / 2;                // workgroups per KV head (256 rows or a pair of half blocks)
@@ -173,8 +336,9 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   const int n_rb_last = a.groups > 1 ? ((a.n_last * r_heads + MF_HB - 1) / MF_HB + 1) / 2 : 0;
   if (a.groups > 1) n_items = n_rb_last + (a.groups - 1) * n_rb;
   // workgroup id -> (KV head, item): ids go round-robin over the 8 XCDs
-  int h, item;
-  {
+  if constexpr (PAGED) {
+    n_items = n_rb;
+  } else {
     const int wg = blockIdx.x, xcd = wg & 7, idx = wg >> 3;
     if (8 % a.h_kv == 0) {
       const int per = 8 / a.h_kv;  // XCDs per KV head
@@ -202,7 +366,11 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   const int tokens = a.n_g;  // of a full group
   size_t t0 = 0;             // first token of this item's group
   int rbi = item, chunk = 0, my_split = 1;  // row block (0 = latest tokens), key chunk, chunks of this row block
-  if (a.groups > 1) {  // from here on: this item's group
+  if constexpr (PAGED) {
+    chunk = a.chunk;
+    my_split = a.n_split;
+    t0 = (size_t)seq.row0;
+  } else if (a.groups > 1) {  // from here on: this item's group
     int grp = a.groups - 1;
     if (item < n_rb_last) {
       a.n_g = a.n_last;
@@ -243,15 +411,15 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   const int t_w_min = min(row0, n_rows - 1) / r_heads;
   const int t_wg_max = min(hb_late * MF_HB + MF_HB - 1, n_rows - 1) / r_heads;
   const bool wave_live = row0 < n_rows && !unpaired;
-  const int n_ct = (a.c + MF_BN - 1) / MF_BN;       // cache tiles
-  const int n_tiles = n_ct + t_wg_max / MF_BN + 1;  // + group tiles
+  const int n_ct = PAGED ? 0 : (a.c + MF_BN - 1) / MF_BN;  // cache tiles
+  const int n_tiles = PAGED ? max(0, base + t_wg_max + MF_BN) / MF_BN : n_ct + t_wg_max / MF_BN + 1;  // + group tiles
   // key split: a chunk walks cache tiles [t_begin, t_end); the last chunk goes on through the group tiles
   const int t_begin = chunk * a.split_tiles;
-  const int t_end = chunk == my_split - 1 ? n_tiles : t_begin + a.split_tiles;
+  const int t_end = PAGED ? min(n_tiles, t_begin + a.split_tiles) : chunk == my_split - 1 ? n_tiles : t_begin + a.split_tiles;
 
   constexpr int CROW = F8 ? MF_D : MF_D * 2;  // bytes of one cached row
-  const unsigned char* ck = (const unsigned char*)a.ck + (size_t)h * a.cap * CROW;
-  const unsigned char* cv = (const unsigned char*)a.cv + (size_t)h * a.cap * CROW;
+  const unsigned char* ck = (const unsigned char*)a.ck + (PAGED ? 0 : (size_t)h * a.cap * CROW);
+  const unsigned char* cv = (const unsigned char*)a.cv + (PAGED ? 0 : (size_t)h * a.cap * CROW);
   const unsigned char* gk = (const unsigned char*)a.k + (t0 * a.h_kv + h) * (MF_D * 2);
   const unsigned char* gv = (const unsigned char*)a.v + (t0 * a.h_kv + h) * (MF_D * 2);
   const unsigned gstride_b = (unsigned)a.h_kv * (MF_D * 2);
@@ -273,7 +441,50 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     unsigned o0, o1, step;
     int tile, event;
   };
-  const int cache_tail = a.c % MF_BN != 0 ? n_ct - 1 : -1;
+  // PAGED: the page numbers of the table's entries from list_first on, one per lane, and which of them are there; what is missing
+  // of the tiles under way, four bits (16 keys each) at 4 * (tile & 7); the eight keys of this wavefront in K's next tile
+  int list = -1, list_first = 0;
+  unsigned long long list_ok = 0;
+  unsigned missing = 0;
+  struct Eight {
+    size_t at;  // byte offset of the first in the pools
+    int left;   // keys behind it up to the last one
+    bool ok;
+  };
+  const int last_key = seq.len - 1;
+  auto eight_keys = [&](int tile) {
+    if constexpr (PAGED) {
+      const int shift = a.pg.page_shift, tile_page = (tile * MF_BN) >> shift;
+      if (tile_page + 3 - list_first >= 64 || tile_page < list_first || list_ok == 0) {
+        list_first = tile_page;
+        list = -1;
+        if (list_first + lane <= last_key >> shift) list = a.pg.table[(size_t)seq_no * a.pg.table_pages + list_first + lane];
+        asm volatile("" : "+v"(list));  // it is waited for here, not in front of every use
+        list_ok = __ballot(paged_page_ok(list, a.pg.n_pages));
+      }
+      unsigned out = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out |= (list_ok >> (((tile * MF_BN + 16 * i) >> shift) - list_first)) & 1 ? 0u : 1u << i;
+      const int sl = 4 * (tile & 7);
+      missing = (missing & ~(15u << sl)) | (out << sl);
+      const int key = min(tile * MF_BN + 8 * wave, last_key & ~7);
+      const int page = __builtin_amdgcn_readlane(list, (key >> shift) - list_first);
+      const bool ok = paged_page_ok(page, a.pg.n_pages);
+      return Eight{paged_row(ok ? page : 0, h, key & ((1 << shift) - 1), a.h_kv, shift) * CROW, last_key - key, ok};
+    } else {
+      return Eight{};
+    }
+  };
+  Eight k_keys{};
+  auto place = [&](Stream& s, const unsigned char* pool, const Eight& e, unsigned c0, unsigned c1) {
+    if constexpr (PAGED) {
+      s.src = e.ok ? pool + e.at : (const unsigned char*)paged_zeros;
+      const int sub = lane >> 4;  // keys past the last one repeat it: masked, never used
+      s.o0 = (unsigned)min(sub, e.left) * CROW + (c0 >> (F8 ? 1 : 0));
+      s.o1 = (unsigned)min(sub + 4, e.left) * CROW + (c1 >> (F8 ? 1 : 0));
+    }
+  };
+  const int cache_tail = PAGED ? -1 : a.c % MF_BN != 0 ? n_ct - 1 : -1;
   const int group_tail = a.n_g % MF_BN != 0 ? n_ct + a.n_g / MF_BN : -1;
   auto settle = [&](Stream& s, const unsigned char* cache, const unsigned char* group, unsigned c0, unsigned c1) {
     const bool in_cache = s.tile < n_ct;
@@ -294,8 +505,29 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   };
   Stream sk, sv;
   sk.tile = sv.tile = t_begin;
-  settle(sk, ck, gk, st_kc0, st_kc1);
-  settle(sv, cv, gv, st_vc0, st_vc1);
+  if constexpr (PAGED) {
+    if (t_begin < t_end) {
+      list_first = (t_begin * MF_BN) >> a.pg.page_shift;
+      k_keys = eight_keys(t_begin);
+      place(sk, ck, k_keys, st_kc0, st_kc1);
+      place(sv, cv, k_keys, st_vc0, st_vc1);
+    }
+  } else {
+    settle(sk, ck, gk, st_kc0, st_kc1);
+    settle(sv, cv, gv, st_vc0, st_vc1);
+  }
+  // K's stream goes on by a tile; V's is one behind it, at the keys that K had
+  auto advance_k = [&]() {
+    if constexpr (PAGED) {
+      if (++sk.tile < t_end) {
+        k_keys = eight_keys(sk.tile);
+        place(sk, ck, k_keys, st_kc0, st_kc1);
+      }
+    } else {
+      advance(sk, ck, gk, st_kc0, st_kc1);
+    }
+  };
+  const int cache_end = PAGED ? t_end : n_ct;  // tiles of an 8-bit cache
   // A pair's four requests: halves of its K tile (0, 1) and of its V tile (2, 3). Tiles of an 8-bit cache cannot go to LDS
   // directly: this lane's 8 bytes of each half are pending in registers until they are stored, widened.
   Pieces pend;
@@ -311,18 +543,18 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     *(u32x4*)(smem + slot * MF_TILE + (i < 2 ? 0 : MF_V0) + (i & 1) * 1024 + wave * 2048 + lane * 16) = widen8(p);
   };
   auto request_k = [&](int slot) {
-    if (F8 && sk.tile < n_ct) pend.p[0] = load_piece(0), pend.p[1] = load_piece(1);
+    if (F8 && sk.tile < cache_end) pend.p[0] = load_piece(0), pend.p[1] = load_piece(1);
     else request_half(0, st_lds + slot * MF_TILE), request_half(1, st_lds + slot * MF_TILE);
   };
   auto request_v = [&](int slot) {
-    if (F8 && sv.tile < n_ct) pend.p[2] = load_piece(2), pend.p[3] = load_piece(3);
+    if (F8 && sv.tile < cache_end) pend.p[2] = load_piece(2), pend.p[3] = load_piece(3);
     else request_half(2, st_lds + slot * MF_TILE), request_half(3, st_lds + slot * MF_TILE);
   };
   auto store_k = [&](int tile, const Pieces& p, int slot) {  // if `tile` is a tile of an 8-bit cache
-    if (F8 && tile < n_ct) store_piece(0, p.p[0], slot), store_piece(1, p.p[1], slot);
+    if (F8 && tile < cache_end) store_piece(0, p.p[0], slot), store_piece(1, p.p[1], slot);
   };
   auto store_v = [&](int tile, const Pieces& p, int slot) {
-    if (F8 && tile < n_ct) store_piece(2, p.p[2], slot), store_piece(3, p.p[3], slot);
+    if (F8 && tile < cache_end) store_piece(2, p.p[2], slot), store_piece(3, p.p[3], slot);
   };
 
   // fragment read addresses (bytes inside a tile)
@@ -360,6 +592,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   float l_run = 0.f;        // this lane's share of the row's denominator
   const float c2 = a.scale_log2;
   float nmc = 0.f;  // -m_run * c2
+  const float lowest = -1e30f / fmaxf(c2, 1.f);  // PAGED: finite, and so is its product with c2
 
   // Moves the reference to the rows' max including this block, rescales what was summed so far and forms the block's
   // numerators (first block of a row, and blocks whose numerators outgrew the reference). look: the max of the tile's other
@@ -374,7 +607,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, other[r]);
     }
     // finite also where every logit so far is -inf: the numerators are 0 then, and the next finite logit moves it again
-    mx = fmaxf(fmaxf(m_run, max_halves(mx)), -FLT_MAX);
+    mx = fmaxf(fmaxf(m_run, max_halves(mx)), PAGED ? lowest : -FLT_MAX);
     const float alpha = __builtin_amdgcn_exp2f((m_run - mx) * c2);
     m_run = mx;
     nmc = -mx * c2;
@@ -386,8 +619,10 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     f32x4 ps = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
-      pack_pair(__builtin_amdgcn_exp2f(fmaf(st[r], c2, nmc)), __builtin_amdgcn_exp2f(fmaf(st[r + 1], c2, nmc)), pf[r >> 3], r & 7);
-      if (r & 2) ps = add_four(pf[r >> 3], (r >> 2) & 1, ps);
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(st[r], c2, nmc)), e1 = __builtin_amdgcn_exp2f(fmaf(st[r + 1], c2, nmc));
+      pack_pair(e0, e1, pf[r >> 3], r & 7);
+      if constexpr (PAGED) ps[0] += e0 + e1;
+      else if (r & 2) ps = add_four(pf[r >> 3], (r >> 2) & 1, ps);
     }
     psum = ps[0];
   };
@@ -403,7 +638,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
                   unsigned turn_mask, bool cut, auto extra) {
     constexpr bool QK = decltype(qk)::value, SECOND = decltype(second)::value;
     constexpr int CUR = SECOND ? 32 * 256 : 0, NEXT = SECOND ? 0 : 32 * 256;
-    float e0 = 0.f, e1 = 0.f;
+    float e0 = 0.f, e1 = 0.f, sum0 = 0.f, sum1 = 0.f;
     f32x16 sn;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sn[r] = 0.f;
@@ -428,6 +663,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
       else do_qk(f);
       if (i & 1) {
         e1 = __builtin_amdgcn_exp2f(t1);
+        if constexpr (PAGED) sum0 += e0, sum1 += e1;
         if (s < 7) t1 = fmaf(s_cur[2 * s + 3], c2, nmc);
         extra(s);
       } else {
@@ -446,11 +682,13 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     if (QK) s_next = sn;
     // behind the step's products: as soon as four were ready, the sums cost 0.3-1 % more
     f32x4 ps0 = {0.f, 0.f, 0.f, 0.f}, ps1 = ps0;
-    ps0 = add_four(p_cur[0], 0, ps0);
-    ps1 = add_four(p_cur[0], 1, ps1);
-    ps0 = add_four(p_cur[1], 0, ps0);
-    ps1 = add_four(p_cur[1], 1, ps1);
-    float psum = ps0[0] + ps1[0];
+    if constexpr (!PAGED) {
+      ps0 = add_four(p_cur[0], 0, ps0);
+      ps1 = add_four(p_cur[0], 1, ps1);
+      ps0 = add_four(p_cur[1], 0, ps0);
+      ps1 = add_four(p_cur[1], 1, ps1);
+    }
+    float psum = PAGED ? sum0 + sum1 : ps0[0] + ps1[0];
     if (__any(psum > MF_RESCALE)) move_reference(s_cur, sn, QK && SECOND && !cut, p_cur, psum);
     l_run += psum;
   };
@@ -476,8 +714,14 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     if (F8 && p < n) store_v(t_begin + p, pend, p & 3);
   };
   auto advance_both = [&]() {
-    advance(sk, ck, gk, st_kc0, st_kc1);
-    advance(sv, cv, gv, st_vc0, st_vc1);
+    if constexpr (PAGED) {
+      ++sv.tile;
+      place(sv, cv, k_keys, st_vc0, st_vc1);
+      advance_k();
+    } else {
+      advance(sk, ck, gk, st_kc0, st_kc1);
+      advance(sv, cv, gv, st_vc0, st_vc1);
+    }
   };
   // All requests of pair p, as far as its tiles exist.
   auto request = [&](int p) {
@@ -487,20 +731,31 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
   };
 
   // Masked tiles: the cache's last one if cut off, and the group's from this wavefront's diagonal on.
-  const int diag_tile = n_ct + (t_w_min + 1) / MF_BN;  // first with keys beyond t_w_min
-  auto masked = [&](int tile) { return tile == cache_tail || tile >= diag_tile; };
+  const int diag_tile = PAGED ? max(0, base + t_w_min + 1) / MF_BN : n_ct + (t_w_min + 1) / MF_BN;  // first with keys beyond t_w_min
+  auto masked = [&](int tile) {
+    if constexpr (PAGED) return tile >= diag_tile || ((missing >> (4 * (tile & 7))) & 15u) != 0;
+    else return tile == cache_tail || tile >= diag_tile;
+  };
   auto mask = [&](f32x16& st, int tile, int kb) {
+    if constexpr (PAGED) {
+      mask_block(st, base + t_lane - tile * MF_BN - 32 * kb - 4 * g);
+      const unsigned out = missing >> (4 * (tile & 7) + 2 * kb);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = (out >> (r >> 3)) & 1 ? -INFINITY : st[r];
+      return;
+    }
     const int lim = tile < n_ct ? a.c - 1 - tile * MF_BN : t_lane - (tile - n_ct) * MF_BN;
     mask_block(st, lim - 32 * kb - 4 * g);
   };
   const bool late = my_split > 1 && a.split_tiles > 2;  // the second and third pair are requested behind the first wait
   // this wavefront's last tile (relative; -1: no rows)
-  const int last = wave_live ? min(n, n_ct + t_w_max / MF_BN + 1 - t_begin) - 1 : -1;
+  const int last = !wave_live ? -1 : PAGED ? max(0, min(n, max(0, base + t_w_max + MF_BN) / MF_BN - t_begin)) - 1
+                                           : min(n, n_ct + t_w_max / MF_BN + 1 - t_begin) - 1;
 
 #pragma unroll
   for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qrow + 16 * s + 8 * g));
-  request_k(3);
-  advance(sk, ck, gk, st_kc0, st_kc1);
+  if (!PAGED || n > 0) request_k(3);
+  advance_k();
   if (F8) {
     // tiles go through registers one after the other; pair 2 stays pending
     const Pieces first = pend;
@@ -509,9 +764,9 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     request(1);
     const Pieces p1 = pend;
     request(2);
-    store_k(t_begin, first, 3);
+    if (!PAGED || n > 0) store_k(t_begin, first, 3);
     if (n > 1) store_k(t_begin + 1, p0, 0);
-    store_v(t_begin, p0, 0);
+    if (!PAGED || n > 0) store_v(t_begin, p0, 0);
     if (n > 2) store_k(t_begin + 2, p1, 1);
     if (n > 1) store_v(t_begin + 1, p1, 1);
   } else {
@@ -567,7 +822,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     // While the pairs to be stored and requested are whole (and, over an 8-bit cache, cache tiles), that work is spread
     // over a step: issued together, the requests hold the wavefront up until the address path has taken those of all
     // wavefronts.
-    const int whole = min(last, (F8 ? min(n, n_ct - t_begin) : n) - 4);
+    const int whole = min(last, (F8 && !PAGED ? min(n, n_ct - t_begin) : n) - 4);
     while (it < whole) {
       const unsigned turn_mask = (it & 1) ? 3 * MF_TILE : MF_TILE;  // slot it & 3 -> slot (it + 1) & 3
       step(true_type(), false_type(), sa, sb, pa, pb, 0u, false, [&](int s) {
@@ -611,6 +866,10 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(AttendArgs a) {
     request(it + 3);
   }
 
+  if constexpr (PAGED) {
+    paged_finish<F8>(a, seq, seq_no, h, chunk, smem, wave, wave_live, row0, n_rows, t_begin * MF_BN, t_end * MF_BN, m_run, l_run, o);
+    return;
+  }
   if (my_split > 1) {
     // partial result of this chunk: every chunk starts on a cache tile, whose keys all rows see, so l_tot > 0
     const bool staged = n_rows > (a.n_g > MF_BN ? MF_HB : MF_DIRECT_ROWS);
@@ -887,10 +1146,9 @@ static void set_lds_limit() {
   static bool attr_set[QP_MAX_DEVICES] = {};
   const int dev = current_device();
   if (dev >= 0 && attr_set[dev]) return;
-  (void)hipFuncSetAttribute((const void*)attend_mfma_kernel<false>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                            MF_LDS);
-  (void)hipFuncSetAttribute((const void*)attend_mfma_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                            MF_LDS);
+  for (const void* f : {(const void*)attend_mfma_kernel<false, AttendArgs>, (const void*)attend_mfma_kernel<true, AttendArgs>,
+                        (const void*)attend_mfma_kernel<false, PagedTileArgs>, (const void*)attend_mfma_kernel<true, PagedTileArgs>})
+    (void)hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, MF_LDS);
   if (dev >= 0) attr_set[dev] = true;
 }
 
@@ -911,9 +1169,9 @@ void launch_attend_mfma_run(const AttendArgs& a_in, hipStream_t s) {
     wgs = (items + per - 1) / per * 8;
   }
   if (a.cache_fp8)
-    hipLaunchKernelGGL(attend_mfma_kernel<true>, dim3((unsigned)wgs), dim3(MF_NT), MF_LDS, s, a);
+    hipLaunchKernelGGL((attend_mfma_kernel<true, AttendArgs>), dim3((unsigned)wgs), dim3(MF_NT), MF_LDS, s, a);
   else
-    hipLaunchKernelGGL(attend_mfma_kernel<false>, dim3((unsigned)wgs), dim3(MF_NT), MF_LDS, s, a);
+    hipLaunchKernelGGL((attend_mfma_kernel<false, AttendArgs>), dim3((unsigned)wgs), dim3(MF_NT), MF_LDS, s, a);
 }
 
 void launch_attend_mfma(const AttendArgs& a_in, void* split_ws, size_t split_ws_bytes, hipStream_t s) {
@@ -932,10 +1190,34 @@ void launch_attend_mfma(const AttendArgs& a_in, void* split_ws, size_t split_ws_
     a.part_lse = a.part_o + (size_t)p.n_split * a.h_kv * a.part_rows * MF_D;
   }
   if (a.cache_fp8)
-    hipLaunchKernelGGL(attend_mfma_kernel<true>, dim3(p.workgroups), dim3(MF_NT), MF_LDS, s, a);
+    hipLaunchKernelGGL((attend_mfma_kernel<true, AttendArgs>), dim3(p.workgroups), dim3(MF_NT), MF_LDS, s, a);
   else
-    hipLaunchKernelGGL(attend_mfma_kernel<false>, dim3(p.workgroups), dim3(MF_NT), MF_LDS, s, a);
+    hipLaunchKernelGGL((attend_mfma_kernel<false, AttendArgs>), dim3(p.workgroups), dim3(MF_NT), MF_LDS, s, a);
   if (p.n_split > 1) launch_attend_merge(a, s);
+}
+
+long long paged_tile_blocks(const PagedArgs& a, const PagedPlan& p) {
+  const long long units = (long long)a.n_seqs * p.chunks;
+  if (8 % a.h_kv == 0) {
+    const int per = 8 / a.h_kv;
+    return (units + per - 1) / per * 8 * p.tiles;
+  }
+  return units * a.h_kv * p.tiles;
+}
+
+void launch_paged_tiles(const PagedArgs& pg, const PagedPlan& p, const void* q, void* out, float* lse, float* part_o, float* part_lse,
+                        hipStream_t s) {
+  set_lds_limit();
+  PagedTileArgs a{};
+  a.q = q, a.out = out, a.lse = lse;
+  a.ck = pg.k, a.cv = pg.v;
+  a.h_q = pg.h_q, a.h_kv = pg.h_kv, a.d = MF_D, a.scale_log2 = pg.scale_log2;
+  a.n_split = p.chunks, a.split_tiles = p.chunks > 1 ? p.chunk_keys / MF_BN : 0x1000000;  // one chunk: all tiles
+  a.part_o = part_o, a.part_lse = part_lse;
+  a.pg = pg, a.row_blocks = p.tiles;
+  const dim3 grid((unsigned)p.workgroups);
+  if (pg.fp8) hipLaunchKernelGGL((attend_mfma_kernel<true, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
+  else hipLaunchKernelGGL((attend_mfma_kernel<false, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
 }
 
 void launch_attend_merge(const AttendArgs& a, hipStream_t s) {

@@ -72,6 +72,11 @@ struct PagedPlan {
 };
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes);
 constexpr size_t PAGED_ATTEND_SCRATCH = (size_t)128 << 20;  // partial results take no more
+// The tile kernel of attend_mfma.hip: 256 stacked rows per workgroup, keys in tiles of 64.
+constexpr int PT_ROWS = 256;
+long long paged_tile_blocks(const PagedArgs& a, const PagedPlan& p);  // workgroups, the padding of the XCD mapping included
+void launch_paged_tiles(const PagedArgs& a, const PagedPlan& p, const void* q, void* out, float* lse, float* part_o, float* part_lse,
+                        hipStream_t s);
 bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, void* out, float* lse, void* scratch,
                          size_t scratch_bytes, hipStream_t s);
 

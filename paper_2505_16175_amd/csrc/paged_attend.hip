@@ -1,6 +1,10 @@
 // Attention of the paged cache's new tokens: online softmax over a sequence's pages.
 //
-// paged_rows_kernel: few stacked rows (tokens x query heads of a KV head; decoding, drafted tokens) against a long axis. What
+// Chunks over bf16 heads of 128 (more than 32 stacked rows of a KV head) run the group attention's tile kernel over the pages
+// (attend_mfma.hip); their chunks are merged here too.
+//
+// paged_rows_kernel: few stacked rows (tokens x query heads of a KV head; decoding, drafted tokens) against a long axis, and
+// other layouts. What
 // bounds it is HBM: K and V are read once and nothing is reused, and the products take a tenth of that time. So there is no LDS
 // tile and no barrier in its loop: a workgroup takes a chunk of a sequence's entries for one KV head, its four wavefronts take
 // blocks of 32 keys (16 of f32) in turn, each straight into registers (paged_rows.h) while the block before it is computed;
@@ -18,8 +22,6 @@ namespace qp {
 constexpr int PR_NW = 4;               // wavefronts per workgroup
 constexpr int PR_LIST = 512;           // page numbers kept in LDS: of a segment of 8192 entries in pages of 16
 constexpr int PR_SEGMENT = PR_LIST * 16;
-constexpr float PR_NONE = -3e38f;      // a row's reference (log2 units) before its first visible entry
-constexpr float PR_LAZY = 8.f;
 
 struct PagedOut {
   const void* q;   // [n_rows][h_q][d]
@@ -28,14 +30,6 @@ struct PagedOut {
   float* part_o;   // [chunks][n_rows * h_q][d], chunks > 1
   float* part_lse; // [chunks][n_rows * h_q], log2 units
   int tiles, chunks, chunk_keys;
-};
-
-template <typename E, int D>
-struct RowsBlock {
-  using L = RowsLayout<E, D>;
-  pr_u32x4 k[L::TILES][L::KL];
-  unsigned v[L::VK][L::VW];
-  int ok;  // bit t: tile t's page is there
 };
 
 // Two workgroups per compute unit where two blocks' rows fit half of the registers.
@@ -66,212 +60,20 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
   if (row0 >= all_rows) return;
   if (chunk > 0 && (long long)chunk * o.chunk_keys >= q.len) return;  // chunk 0 always answers
   const int n_rows = (int)(all_rows - row0 < ROWS ? all_rows - row0 : ROWS);
-  // what the tile's rows see: the first of them least, the last most
-  const int lim_min = q.base + row0 / r_heads, lim_max = q.base + (row0 + n_rows - 1) / r_heads;
+  const int lim_max = q.base + (row0 + n_rows - 1) / r_heads;  // the last row sees most
   const int k_begin = chunk * o.chunk_keys;
   const int k_end = min(min(q.len, lim_max + 1), o.chunk_keys < q.len - k_begin ? k_begin + o.chunk_keys : q.len);
 
-  int lim[RT];  // of this lane's row
-  pr_u32x4 qf[RT][L::QF];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int row = row0 + min(16 * t + l16, n_rows - 1), i = row / r_heads;
-    lim[t] = q.base + i;
-    const unsigned char* p = (const unsigned char*)o.q +
-                             ((size_t)(q.row0 + i) * a.h_q + (size_t)h * r_heads + (row - i * r_heads)) * (D * L::QB);
-#pragma unroll
-    for (int u = 0; u < L::QF; ++u) qf[t][u] = *(const pr_u32x4*)(p + rows_q_byte<E, D>(u, g));
-  }
-  pr_f32x4 acc[RT][NE];
-  float m[RT], l[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    m[t] = PR_NONE;
-    l[t] = 0.f;
-#pragma unroll
-    for (int e = 0; e < NE; ++e) acc[t][e] = pr_f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  RowsWave<E, D, RT> rows;
+  rows.init(a, q, o.q, h, row0, n_rows);
   const float c2 = a.scale_log2;
-  const int mask = (1 << a.page_shift) - 1;
   int seg = k_begin;  // first entry of the segment whose pages are listed
 
   auto load = [&](Block& b, int key0) {
-    b.ok = 0;
-#pragma unroll
-    for (int t = 0; t < L::TILES; ++t) {
-      const int key = key0 + 16 * t;
-      // a tile past the last entry takes the block's first page: read, never used
-      const int page = __builtin_amdgcn_readfirstlane(pages[((key < k_end ? key : key0) >> a.page_shift) - (seg >> a.page_shift)]);
-      const bool ok = paged_page_ok(page, a.n_pages);
-      b.ok |= ok && key < k_end ? 1 << t : 0;
-      const size_t at = paged_row(ok ? page : 0, h, key & mask, a.h_kv, a.page_shift) * L::ROWB;
-      rows_load_k<E, D>((const unsigned char*)a.k + at, l16, g, b.k[t]);
-      const unsigned char* vb = (const unsigned char*)a.v + at;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const unsigned off = (unsigned)((4 * g + r) * L::ROWB + l16 * (NE * (int)sizeof(E)));
-        if constexpr (L::VW == 2) {
-          const uint2 raw = *(const uint2*)(vb + off);
-          b.v[4 * t + r][0] = raw.x, b.v[4 * t + r][1] = raw.y;
-        } else {
-#pragma unroll
-          for (int w = 0; w < L::VW; w += 4) {
-            const pr_u32x4 raw = *(const pr_u32x4*)(vb + (off + 4 * w));
-#pragma unroll
-            for (int y = 0; y < 4; ++y) b.v[4 * t + r][w + y] = raw[y];
-          }
-        }
-      }
-    }
+    rows.load(b, a, h, key0, k_end,
+              [&](int key) { return __builtin_amdgcn_readfirstlane(pages[(key >> a.page_shift) - (seg >> a.page_shift)]); });
   };
-
-  auto compute = [&](Block& b, int key0) {
-    if (b.ok == 0) return;
-    const bool whole = b.ok == (1 << L::TILES) - 1 && key0 + L::BK <= k_end && key0 + L::BK - 1 <= lim_min;
-    if (!whole) {
-      // V of entries that are not there may hold anything: 0 times it is not 0
-#pragma unroll
-      for (int j = 0; j < L::VK; ++j) {
-        const bool there = ((b.ok >> (j >> 2)) & 1) && key0 + 16 * (j >> 2) + 4 * g + (j & 3) < k_end;
-#pragma unroll
-        for (int w = 0; w < L::VW; ++w) b.v[j][w] = there ? b.v[j][w] : 0u;
-      }
-    }
-    float p[RT][L::VK];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-      for (int y = 0; y < L::TILES; ++y) {
-        const pr_f32x4 st = rows_products<E, D, true>(b.k[y], qf[t]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const bool seen = whole || (((b.ok >> y) & 1) && key0 + 16 * y + 4 * g + r <= min(lim[t], k_end - 1));
-          p[t][4 * y + r] = seen ? st[r] : -INFINITY;
-        }
-      }
-      float mx = p[t][0];
-#pragma unroll
-      for (int j = 1; j < L::VK; ++j) mx = fmaxf(mx, p[t][j]);
-      mx *= c2;
-      if (__any(mx > m[t] + PR_LAZY)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(fmaxf(mx, __shfl_xor(mx, 32, 64)), m[t]);
-        const float alpha = __builtin_amdgcn_exp2f(m[t] - mx);
-        m[t] = mx;
-        l[t] *= alpha;
-#pragma unroll
-        for (int e = 0; e < NE; ++e)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[t][e][r] *= alpha;
-      }
-#pragma unroll
-      for (int j = 0; j < L::VK; ++j) {
-        p[t][j] = __builtin_amdgcn_exp2f(fmaf(p[t][j], c2, -m[t]));
-        l[t] += p[t][j];
-      }
-    }
-    const pr_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (L::F32) {
-      bool bad = false;
-      if (!whole) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) bad = bad || pr_not_finite(__uint_as_float(b.v[r][e]));
-      }
-      if (__any(bad)) {
-#pragma unroll
-        for (int e = 0; e < NE; ++e)
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            pr_f32x4 plus = zero, minus = zero;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const Split v = pr_split(__uint_as_float(b.v[r][e]));
-              acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.finite, p[t][r], acc[t][e], 0, 0, 0);
-              plus = __builtin_amdgcn_mfma_f32_16x16x4f32(v.plus, p[t][r], plus, 0, 0, 0);
-              minus = __builtin_amdgcn_mfma_f32_16x16x4f32(v.minus, p[t][r], minus, 0, 0, 0);
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float z = acc[t][e][r];
-              pr_join(z, plus[r], minus[r]);
-              acc[t][e][r] = z;
-            }
-          }
-        return;
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int e = 0; e < NE; ++e)
-#pragma unroll
-          for (int t = 0; t < RT; ++t)
-            acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.v[r][e]), p[t][r], acc[t][e], 0, 0, 0);
-    } else {
-      pr_bf16x8 hi[RT], lo[RT];
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          hi[t][j] = (__bf16)p[t][j];
-          lo[t][j] = (__bf16)(p[t][j] - (float)hi[t][j]);
-        }
-      unsigned w[8][NE / 2];  // V as pairs of bf16
-      bool bad = false;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (L::F8) {
-          const pr_u32x4 z = pr_widen8(b.v[j][0], b.v[j][1]);
-#pragma unroll
-          for (int y = 0; y < 4; ++y) w[j][y] = z[y];
-        } else {
-#pragma unroll
-          for (int y = 0; y < NE / 2; ++y) w[j][y] = b.v[j][y];
-        }
-        if (!whole) {
-#pragma unroll
-          for (int y = 0; y < NE / 2; ++y)
-            bad = bad || pr_not_finite(bf16lo_to_f32(w[j][y])) || pr_not_finite(bf16hi_to_f32(w[j][y]));
-        }
-      }
-      const bool guard = __any(bad);
-#pragma unroll
-      for (int e = 0; e < NE; ++e) {
-        pr_u32x4 f;  // element e of the lane's 8 keys
-#pragma unroll
-        for (int y = 0; y < 4; ++y)
-          f[y] = __builtin_amdgcn_perm(w[2 * y + 1][e >> 1], w[2 * y][e >> 1], (e & 1) ? 0x07060302u : 0x05040100u);
-        if (guard) {
-          pr_u32x4 finite, fp, fm;
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            unsigned x0, x1, x2;
-            pr_split_pair(f[y], x0, x1, x2);
-            finite[y] = x0, fp[y] = x1, fm[y] = x2;
-          }
-          f = finite;
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const pr_f32x4 plus = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, fp), hi[t], zero, 0, 0, 0);
-            const pr_f32x4 minus = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, fm), hi[t], zero, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float z = acc[t][e][r];
-              pr_join(z, plus[r], minus[r]);
-              acc[t][e][r] = z;
-            }
-          }
-        }
-        const pr_bf16x8 vf = __builtin_bit_cast(pr_bf16x8, f);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[t], acc[t][e], 0, 0, 0);
-          acc[t][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[t], acc[t][e], 0, 0, 0);
-        }
-      }
-    }
-  };
+  auto compute = [&](Block& b, int key0) { rows.compute(b, key0, k_end, c2); };
 
   for (; seg < k_end; seg += PR_SEGMENT) {
     const int seg_end = min(k_end, k_end - seg > PR_SEGMENT ? seg + PR_SEGMENT : k_end);
@@ -297,10 +99,9 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
   // the wavefronts' results meet in LDS
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    float z = l[t] + __shfl_xor(l[t], 16, 64);
-    z += __shfl_xor(z, 32, 64);
+    const float z = rows.denominator(t);
     if (g == 0) {
-      sm_m[wave][16 * t + l16] = m[t];
+      sm_m[wave][16 * t + l16] = rows.m[t];
       sm_l[wave][16 * t + l16] = z;
     }
     float* const to = &slab[wave][16 * t + l16][4 * NE * g];
@@ -308,7 +109,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int e = 0; e < NE; e += 4)
-        *(float4*)(to + NE * r + e) = make_float4(acc[t][e][r], acc[t][e + 1][r], acc[t][e + 2][r], acc[t][e + 3][r]);
+        *(float4*)(to + NE * r + e) = make_float4(rows.acc[t][e][r], rows.acc[t][e + 1][r], rows.acc[t][e + 2][r], rows.acc[t][e + 3][r]);
   }
   __syncthreads();
   const size_t total = (size_t)a.n_rows * a.h_q;
@@ -441,28 +242,33 @@ static long long merge_blocks(const PagedArgs& a, int chunks) {
   return (((long long)a.max_new * a.h_q + rows - 1) / rows) * a.n_seqs;
 }
 
+// Stacked rows above which bf16 heads of 128 take the tile kernel (attend_mfma.hip), and what its 32-bit arithmetic takes.
+constexpr long long PT_FROM_ROWS = 32, PT_MOST_ROWS = 1 << 26;
+
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes) {
   PagedPlan p{};
   const long long rows = (long long)a.max_new * (a.h_q / a.h_kv);
-  const int bk = dtype == QP_F32 ? 16 : 32;
-  p.tile_rows = rows <= 16 ? 16 : 32;
+  const bool tiled = dtype == QP_BF16 && d == 128 && rows > PT_FROM_ROWS && rows <= PT_MOST_ROWS;
+  const int step = tiled ? 64 : PR_NW * (dtype == QP_F32 ? 16 : 32);  // entries of a chunk are a multiple of it
+  p.tile_rows = tiled ? PT_ROWS : rows <= 16 ? 16 : 32;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   const long long units = (long long)a.n_seqs * a.h_kv * p.tiles;
-  // About two workgroups per compute unit and twice that for the shorter sequences; at least two blocks per wavefront.
+  // Rows: about two workgroups per compute unit and twice that for the shorter sequences; at least two blocks per wavefront.
+  // Tiles, one workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys.
   const long long want = std::max<long long>(1, (4ll * device_cu_count() + units - 1) / units);
-  const long long least = 2 * PR_NW * bk;
-  long long keys = std::max<long long>(((a.max_len + want - 1) / want + PR_NW * bk - 1) / (PR_NW * bk) * (PR_NW * bk), least);
+  const long long least = tiled ? 16 * 64 : 2 * step;
+  long long keys = std::max<long long>(((a.max_len + want - 1) / want + step - 1) / step * step, least);
   const size_t per_chunk = (size_t)a.n_rows * a.h_q * (d + 1) * sizeof(float);
   long long chunks = (a.max_len + keys - 1) / keys;
   const long long fit = (long long)(std::min(scratch_bytes, PAGED_ATTEND_SCRATCH) / per_chunk);
   if (chunks > fit) {
     chunks = fit >= 2 ? fit : 1;
-    keys = ((a.max_len + chunks - 1) / chunks + bk - 1) / bk * bk;
+    keys = ((a.max_len + chunks - 1) / chunks + step - 1) / step * step;
     chunks = (a.max_len + keys - 1) / keys;
   }
   p.chunks = (int)std::max<long long>(chunks, 1);
   p.chunk_keys = (int)std::min<long long>(keys, 0x40000000);
-  p.workgroups = units * p.chunks;
+  p.workgroups = tiled ? paged_tile_blocks(a, p) : units * p.chunks;
   p.scratch_bytes = p.chunks > 1 ? per_chunk * p.chunks : 0;
   return p;
 }
@@ -470,7 +276,8 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
 template <typename E, typename T, int D>
 static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p, hipStream_t s) {
   const dim3 grid((unsigned)p.workgroups), block(PR_NW * 64);
-  if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1>), grid, block, 0, s, a, o);
+  if (p.tile_rows == PT_ROWS) launch_paged_tiles(a, p, o.q, o.out, o.lse, o.part_o, o.part_lse, s);
+  else if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1>), grid, block, 0, s, a, o);
   else hipLaunchKernelGGL((paged_rows_kernel<E, D, 2>), grid, block, 0, s, a, o);
   if (p.chunks > 1) {
     const dim3 merge((unsigned)merge_blocks(a, p.chunks));
@@ -483,7 +290,7 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
 bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, void* out, float* lse, void* scratch,
                          size_t scratch_bytes, hipStream_t s) {
   const PagedPlan p = plan_paged_attend(a, dtype, d, scratch != nullptr ? scratch_bytes : 0);
-  if (p.workgroups * PR_NW * 64 > PAGED_MAX_THREADS || merge_blocks(a, p.chunks) * PM_SHARE * 64 > PAGED_MAX_THREADS) return false;
+  if (p.workgroups * (p.tile_rows == PT_ROWS ? 512 : PR_NW * 64) > PAGED_MAX_THREADS || merge_blocks(a, p.chunks) * PM_SHARE * 64 > PAGED_MAX_THREADS) return false;
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;

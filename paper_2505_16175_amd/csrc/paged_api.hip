@@ -83,7 +83,11 @@ size_t qp_paged_workspace_bytes(const qp_layout* L, int32_t n_seqs, int32_t n_ro
     qp::PagedArgs a{};
     a.n_seqs = n_seqs, a.n_rows = n_rows, a.max_new = max_new < n_rows ? max_new : n_rows, a.max_len = max_len;
     a.h_q = L->n_q_heads, a.h_kv = L->n_kv_heads, a.page_shift = 8;
-    const size_t attend = qp::plan_paged_attend(a, L->dtype, L->head_dim, qp::PAGED_ATTEND_SCRATCH).scratch_bytes;
+    size_t attend = 0;  // over a pool of either format
+    for (a.fp8 = 0; a.fp8 < 2; ++a.fp8) {
+      const size_t x = qp::plan_paged_attend(a, L->dtype, L->head_dim, qp::PAGED_ATTEND_SCRATCH).scratch_bytes;
+      attend = x > attend ? x : attend;
+    }
     const size_t weigh = qp::paged_weigh_workspace_bytes(n_seqs, a.h_q, a.h_kv, a.max_new, max_len);
     most = attend > most ? attend : most;
     most = weigh > most ? weigh : most;

@@ -253,9 +253,13 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   p.tile_rows = tiled ? PT_ROWS : rows <= 16 ? 16 : 32;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   const long long units = (long long)a.n_seqs * a.h_kv * p.tiles;
-  // Rows: about two workgroups per compute unit and twice that for the shorter sequences; at least two blocks per wavefront.
-  // Tiles, one workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys.
-  const long long want = std::max<long long>(1, (4ll * device_cu_count() + units - 1) / units);
+  // Rows: one workgroup per compute unit, two over 8-bit pools, of at least two blocks per wavefront. us by workgroups per compute
+  // unit 1 / 2 / 4: one token of the 7B heads over 46,125 entries 25.0 / 27.6 / 30.1, of 32 sequences over up to 9,840 84.8 / 89.8 /
+  // 93.2; up to four of the 72B heads of 16 sequences over 8-bit pages of up to 32,768 251 / 180 / 187.
+  // Tiles, one workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys (four questions of up to
+  // 300 tokens over up to 46,125 entries, one round 544, two 580, three 555, four 506, six 531).
+  const int rounds = tiled ? 4 : a.fp8 ? 2 : 1;
+  const long long want = std::max<long long>(1, ((long long)rounds * device_cu_count() + units - 1) / units);
   const long long least = tiled ? 16 * 64 : 2 * step;
   long long keys = std::max<long long>(((a.max_len + want - 1) / want + step - 1) / step * step, least);
   const size_t per_chunk = (size_t)a.n_rows * a.h_q * (d + 1) * sizeof(float);

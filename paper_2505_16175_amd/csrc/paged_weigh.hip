@@ -48,8 +48,15 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
     rows_load_k<E, D>((const unsigned char*)a.k + at, l16, g, k[t]);
   }
   float w[KT];
+  float* to[KT];  // group g stores tile g: what was there is requested with the keys
+  float before = 0.f;
 #pragma unroll
-  for (int t = 0; t < KT; ++t) w[t] = 0.f;
+  for (int t = 0; t < KT; ++t) {
+    w[t] = 0.f;
+    const int key = key0 + 16 * t + l16;
+    to[t] = a.weight + paged_row(max(page[t], 0), h, key & mask, a.h_kv, a.page_shift);
+    if (accumulate && g == t && page[t] >= 0 && key < q.len) before = *to[t];
+  }
   const long long all_rows = (long long)q.n * r_heads;
   const float c2 = a.scale_log2;
   const int last = key0 + 16 * KT - 1;
@@ -93,10 +100,7 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
     w[t] += __shfl_xor(w[t], 16, 64);
     w[t] += __shfl_xor(w[t], 32, 64);
     const int key = key0 + 16 * t + l16;
-    if (g == t && page[t] >= 0 && key < q.len) {
-      float* const to = a.weight + paged_row(page[t], h, key & mask, a.h_kv, a.page_shift);
-      *to = accumulate ? *to + w[t] : w[t];
-    }
+    if (g == t && page[t] >= 0 && key < q.len) *to[t] = before + w[t];
   }
 }
 
@@ -188,19 +192,6 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
     __syncthreads();  // the last segment's statistics and slots have been read
     if (tid < WT_ROWS / 32) dead[tid] = 0;
     __syncthreads();
-    for (int r = tid; r < (seg_end - seg) * 32; r += WT_NW * 64) {
-      float v = -INFINITY;
-      if (row0 + r < rows) {
-        const int t = (row0 + r) / r_heads, j = row0 + r - t * r_heads;
-        const float z = o.lse[(size_t)(h * r_heads + j) * a.n_rows + q.row0 + t];
-        v = -z * 1.4426950408889634f;
-        if (z == -INFINITY) {
-          v = -INFINITY;
-          dead[r >> 5] = 1;
-        }
-      }
-      neg[r] = v;
-    }
     // queries: request i of a wavefront fills rows 8 wave + 4 i + (lane >> 4) of a slot, chunk lane & 15 of each from where the swizzle
     // has it; a row's offset goes on by 32 rows from tile to tile
     const int t_seg = row0 / r_heads;
@@ -232,6 +223,31 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
 #pragma unroll
     for (int i = 0; i < 3; ++i)
       if (i < n) request(i);
+    // the rows' statistics, six loads of a thread under way together
+    {
+      constexpr int STEP = WT_NW * 64, B = 6;
+      const int rows_here = (seg_end - seg) * 32;
+      int t = (row0 + tid) / r_heads, j = row0 + tid - t * r_heads;
+      const int dt = STEP / r_heads, dj = STEP % r_heads;
+      for (int r0 = tid; r0 < rows_here; r0 += B * STEP) {
+        float z[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+          const int r = r0 + u * STEP;
+          z[u] = r < rows_here && row0 + r < rows ? o.lse[(size_t)(h * r_heads + j) * a.n_rows + q.row0 + t] : -INFINITY;
+          t += dt;
+          j += dj;
+          if (j >= r_heads) j -= r_heads, ++t;
+        }
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+          const int r = r0 + u * STEP;
+          if (r >= rows_here) continue;
+          neg[r] = z[u] == -INFINITY ? -INFINITY : -z[u] * 1.4426950408889634f;
+          if (z[u] == -INFINITY && row0 + r < rows) dead[r >> 5] = 1;
+        }
+      }
+    }
     for (int i = 0; i < n; ++i) {
       // tile i is there: two more may be under way. The statistics' loads were waited for by the compiler.
       if (i + 2 < n) weigh_wait<4>();

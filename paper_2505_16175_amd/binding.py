@@ -489,19 +489,29 @@ class Feed:
 
 
 # ---- the paged cache (include/qp_paged.h) ----
+# A decoding step's calls are a few microseconds of GPU work, so what the host spends on one counts: what does not change from call to
+# call (the structs' references) is kept with its owner, and a tensor is looked at once.
 
-def _on_device(*tensors):
-    """Calls run on the current device: a tensor of another one would be read across the link, or not at all."""
-    here = torch.cuda.current_device() if _device is None else _device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError("expected tensors of the current GPU")
+def _here():
+    return torch.cuda.current_device() if _device is None else _device()
 
 
-def _typed(t, dtype, shape, name):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+def _dense(t, dtype, shape, name, here):
+    """The address of a dense tensor of that type and shape on the current device (one of another device would be read across the
+    link, or not at all)."""
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return t
+    if t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of the current GPU")
+    return t.data_ptr()
+
+
+def _scratch(workspace, here):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != here or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor of the current GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _layout_dtype(layout):
@@ -520,13 +530,17 @@ class PagedCache:
         if k is not None and k.dtype == torch.float8_e4m3fn:
             fmt = QP_CACHE_FP8_E4M3
         dt = torch.float8_e4m3fn if fmt == QP_CACHE_FP8_E4M3 else _layout_dtype(layout)
-        new = lambda t, shape, dtype, name: torch.zeros(shape, dtype=dtype, device=device) if t is None else _typed(t, dtype, shape, name)
-        self.k = new(k, (*rows, layout.head_dim), dt, "k")
-        self.v = new(v, (*rows, layout.head_dim), dt, "v")
-        self.pos = torch.full(rows, -1, dtype=torch.int32, device=device) if pos is None else _typed(pos, torch.int32, rows, "pos")
-        self.weight = new(weight, rows, torch.float32, "weight") if weights or weight is not None else None
-        _on_device(self.k, self.v, self.pos, self.weight)
-        self.c = qp_paged_cache(_ptr(self.k), _ptr(self.v), _ptr(self.pos), _ptr(self.weight), n_pages, page_tokens, fmt)
+        self.k = torch.zeros(*rows, layout.head_dim, dtype=dt, device=device) if k is None else k
+        self.v = torch.zeros(*rows, layout.head_dim, dtype=dt, device=device) if v is None else v
+        self.pos = torch.full(rows, -1, dtype=torch.int32, device=device) if pos is None else pos
+        self.weight = torch.zeros(rows, dtype=torch.float32, device=device) if weights and weight is None else weight
+        here = self.k.get_device()
+        at = [_dense(t, d, (*rows, layout.head_dim) if t is self.k or t is self.v else rows, name, here)
+              for t, d, name in ((self.k, dt, "k"), (self.v, dt, "v"), (self.pos, torch.int32, "pos"))]
+        at.append(None if self.weight is None else _dense(self.weight, torch.float32, rows, "weight", here))
+        self.device_index = here
+        self.c = qp_paged_cache(*at, n_pages, page_tokens, fmt)
+        self.ref = ctypes.byref(self.c)
 
 
 class PagedBatch:
@@ -535,22 +549,32 @@ class PagedBatch:
     launched; by default every row may belong to one sequence, and a sequence may fill its table."""
 
     def __init__(self, page_table, length, row_start=None, n_rows=0, max_new=None, max_len=None):
-        if page_table.dim() != 2 or page_table.dtype != torch.int32:
+        here = page_table.get_device()
+        if page_table.dim() != 2:
             raise ValueError("page_table: expected int32 [n_seqs][pages]")
         n_seqs = page_table.shape[0]
-        _typed(length, torch.int32, (n_seqs,), "length")
-        if row_start is not None:
-            _typed(row_start, torch.int32, (n_seqs + 1,), "row_start")
-        _on_device(page_table, length, row_start)
+        at = [_dense(page_table, torch.int32, page_table.shape, "page_table", here),
+              _dense(length, torch.int32, (n_seqs,), "length", here),
+              None if row_start is None else _dense(row_start, torch.int32, (n_seqs + 1,), "row_start", here)]
+        if here < 0:
+            raise ValueError("page_table: expected a tensor on the GPU")
         self.page_table, self.length, self.row_start, self.max_len = page_table, length, row_start, max_len
-        self.c = qp_paged_batch(_ptr(page_table), _ptr(length), _ptr(row_start), n_seqs, page_table.shape[1], n_rows,
-                                n_rows if max_new is None else max_new, 0)
+        self.n_seqs, self.n_rows, self.device_index = n_seqs, n_rows, here
+        self.c = qp_paged_batch(*at, n_seqs, page_table.shape[1], n_rows, n_rows if max_new is None else max_new, max_len or 0)
+        self.ref = ctypes.byref(self.c)
 
-    def of(self, page_tokens):
-        """The struct for a pool of such pages."""
-        most = min(self.c.table_pages * page_tokens, 1 << 30)
-        self.c.max_len = most if self.max_len is None else self.max_len
-        return ctypes.byref(self.c)
+    def of(self, cache):
+        """The struct for a pool, whose pages say what a sequence of the batch can hold where it states no max_len."""
+        if self.max_len is None:
+            self.c.max_len = min(self.c.table_pages * cache.c.page_tokens, 1 << 30)
+        return self.ref
+
+
+def _same_gpu(cache, batch):
+    here = _here()
+    if cache.device_index != here or batch.device_index != here:
+        raise ValueError("expected a cache and a batch of the current GPU")
+    return here
 
 
 def paged_workspace_bytes(layout, n_seqs, n_rows, max_new, max_len, keep=0) -> int:
@@ -559,79 +583,76 @@ def paged_workspace_bytes(layout, n_seqs, n_rows, max_new, max_len, keep=0) -> i
 
 def make_paged_workspace(layout, batch: PagedBatch, keep=0, page_tokens=256, device="cuda") -> torch.Tensor:
     """Scratch for every paged call of the batch's sizes (page_tokens: needed where the batch states no max_len)."""
-    batch.of(page_tokens)
-    n = paged_workspace_bytes(layout, batch.c.n_seqs, batch.c.n_rows, batch.c.max_new, batch.c.max_len, keep)
+    max_len = min(batch.c.table_pages * page_tokens, 1 << 30) if batch.max_len is None else batch.max_len
+    n = paged_workspace_bytes(layout, batch.n_seqs, batch.n_rows, batch.c.max_new, max_len, keep)
     if n == 0:
         raise QPError(QP_ERR_INVALID_ARG, "qp_paged_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device)
-
-
-def _rows_of(layout, batch, q, heads, name):
-    return _typed(q, _layout_dtype(layout), (batch.c.n_rows, heads, layout.head_dim), name)
 
 
 def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
     """k, v [n_rows][H_kv][d] of any strides whose rows are runs of d elements (a flat cache's [H_kv][capacity][d] comes as
     k.transpose(0, 1)[:n]); pos int32 [n_rows], or [n_rows][H_kv] with a position per head. Rows of an 8-bit pool may be
     torch.float8_e4m3fn already."""
-    raw = k.dtype == torch.float8_e4m3fn
-    shape = (batch.c.n_rows, layout.n_kv_heads, layout.head_dim)
-    dt = torch.float8_e4m3fn if raw else _layout_dtype(layout)
-    _typed(k, dt, shape, "k")
-    _typed(v, dt, shape, "v")
-    _on_device(k, v, pos, cache.k, batch.page_table)
-    steps = [tuple(0 if n == 1 else x for n, x in zip(shape, t.stride())) for t in (k, v)]  # of one row, any stride does
-    if steps[0] != steps[1] or steps[0][2] != 1:
+    here = _same_gpu(cache, batch)
+    n, h_kv, d = batch.n_rows, layout.n_kv_heads, layout.head_dim
+    shape, dt = (n, h_kv, d), k.dtype
+    raw = dt is torch.float8_e4m3fn
+    if not raw and dt is not _layout_dtype(layout) or v.dtype is not dt or k.shape != shape or v.shape != shape:
+        raise ValueError(f"k and v: expected {_layout_dtype(layout)} {shape}, got {dt} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
+    sk, sv = k.stride(), v.stride()
+    if n == 1 or h_kv == 1:                              # of one row, any stride does
+        sk, sv = ((0 if n == 1 else s[0], 0 if h_kv == 1 else s[1], s[2]) for s in (sk, sv))
+    if sk != sv or sk[2] != 1:
         raise ValueError("k and v: expected the same strides and rows in one run")
-    if pos.dtype != torch.int32 or tuple(pos.shape) not in (shape[:1], shape[:2]):
+    if pos.dtype is not torch.int32 or pos.shape != shape[:1] and pos.shape != shape[:2]:
         raise ValueError("pos: expected int32 [n_rows] or [n_rows][H_kv]")
-    st = lib().qp_paged_append(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), k.data_ptr(),
-                               v.data_ptr(), steps[0][0], steps[0][1], pos.data_ptr(), pos.stride(0),
-                               pos.stride(1) if pos.dim() == 2 else 0, QP_CACHE_FP8_E4M3 if raw else QP_CACHE_SAME, _stream())
+    if k.get_device() != here or v.get_device() != here or pos.get_device() != here:
+        raise ValueError("expected tensors of the current GPU")
+    sp = pos.stride()
+    st = lib().qp_paged_append(ctypes.byref(layout), cache.ref, batch.of(cache), k.data_ptr(), v.data_ptr(), sk[0], sk[1],
+                               pos.data_ptr(), sp[0], sp[1] if len(sp) == 2 else 0, QP_CACHE_FP8_E4M3 if raw else QP_CACHE_SAME,
+                               _stream())
     _check(st, "qp_paged_append")
 
 
 def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None, workspace=None):
     """q, out [n_rows][H_q][d], lse float32 [H_q][n_rows]."""
-    _rows_of(layout, batch, q, layout.n_q_heads, "q")
-    _rows_of(layout, batch, out, layout.n_q_heads, "out")
-    if lse is not None:
-        _typed(lse, torch.float32, (layout.n_q_heads, batch.c.n_rows), "lse")
-    _on_device(q, out, lse, workspace, cache.k, batch.page_table)
-    wp, wb = _ws(workspace)
-    st = lib().qp_paged_attend(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), _ptr(q), _ptr(out),
-                               _ptr(lse), wp, wb, _stream())
+    here = _same_gpu(cache, batch)
+    dt, shape = _layout_dtype(layout), (batch.n_rows, layout.n_q_heads, layout.head_dim)
+    wp, wb = _scratch(workspace, here)
+    st = lib().qp_paged_attend(ctypes.byref(layout), cache.ref, batch.of(cache), _dense(q, dt, shape, "q", here),
+                               _dense(out, dt, shape, "out", here),
+                               None if lse is None else _dense(lse, torch.float32, (shape[1], shape[0]), "lse", here), wp, wb, _stream())
     _check(st, "qp_paged_attend")
 
 
 def paged_weigh(layout, cache: PagedCache, batch: PagedBatch, q, lse, accumulate=True, workspace=None):
     """Adds to (or, accumulate=False, writes) cache.weight what the batch's rows of paged_attend's lse looked at."""
-    _rows_of(layout, batch, q, layout.n_q_heads, "q")
-    _typed(lse, torch.float32, (layout.n_q_heads, batch.c.n_rows), "lse")
-    _on_device(q, lse, workspace, cache.k, batch.page_table)
-    wp, wb = _ws(workspace)
-    st = lib().qp_paged_weigh(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), _ptr(q), _ptr(lse),
-                              int(accumulate), wp, wb, _stream())
+    here = _same_gpu(cache, batch)
+    shape = (batch.n_rows, layout.n_q_heads, layout.head_dim)
+    wp, wb = _scratch(workspace, here)
+    st = lib().qp_paged_weigh(ctypes.byref(layout), cache.ref, batch.of(cache), _dense(q, _layout_dtype(layout), shape, "q", here),
+                              _dense(lse, torch.float32, (shape[1], shape[0]), "lse", here), 1 if accumulate else 0, wp, wb, _stream())
     _check(st, "qp_paged_weigh")
 
 
 def paged_evict(layout, cache: PagedCache, batch: PagedBatch, keep, n_first, n_last, to_table, to_len, kept=None, workspace=None):
     """to_table int32 [n_seqs][pages], to_len int32 [n_seqs], kept int32 [n_seqs][H_kv][keep] or None."""
-    n_seqs = batch.c.n_seqs
-    if to_table.dim() != 2 or to_table.dtype != torch.int32 or to_table.shape[0] != n_seqs:
+    here = _same_gpu(cache, batch)
+    n_seqs = batch.n_seqs
+    if to_table.dim() != 2 or to_table.shape[0] != n_seqs:
         raise ValueError("to_table: expected int32 [n_seqs][pages]")
-    _typed(to_len, torch.int32, (n_seqs,), "to_len")
-    if kept is not None:
-        _typed(kept, torch.int32, (n_seqs, layout.n_kv_heads, keep), "kept")
-    _on_device(to_table, to_len, kept, workspace, cache.k, batch.page_table)
-    wp, wb = _ws(workspace)
-    st = lib().qp_paged_evict(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), keep, n_first, n_last,
-                              _ptr(to_table), to_table.shape[1], _ptr(to_len), _ptr(kept), wp, wb, _stream())
+    wp, wb = _scratch(workspace, here)
+    st = lib().qp_paged_evict(ctypes.byref(layout), cache.ref, batch.of(cache), keep, n_first, n_last,
+                              _dense(to_table, torch.int32, to_table.shape, "to_table", here), to_table.shape[1],
+                              _dense(to_len, torch.int32, (n_seqs,), "to_len", here),
+                              None if kept is None else _dense(kept, torch.int32, (n_seqs, layout.n_kv_heads, keep), "kept", here),
+                              wp, wb, _stream())
     _check(st, "qp_paged_evict")
 
 
 def paged_plan(layout, cache: PagedCache, batch: PagedBatch, workspace_bytes=0) -> dict:
     info = qp_paged_plan_info()
-    _check(lib().qp_paged_plan(ctypes.byref(layout), ctypes.byref(cache.c), batch.of(cache.c.page_tokens), workspace_bytes,
-                               ctypes.byref(info)), "qp_paged_plan")
+    _check(lib().qp_paged_plan(ctypes.byref(layout), cache.ref, batch.of(cache), workspace_bytes, ctypes.byref(info)), "qp_paged_plan")
     return {name: getattr(info, name) for name, _ in qp_paged_plan_info._fields_}

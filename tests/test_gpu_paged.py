@@ -315,6 +315,20 @@ def test_append(layout, page, fp8, lens, new, missing, source):
         np.testing.assert_array_equal(got[name], want[name], err_msg=name)
 
 
+def test_append_rounds_every_bf16_as_the_flat_cache_does():
+    """All 65,536 patterns, infinities and NaN of both signs among them, against the library's own routine on the host."""
+    layout = B.make_layout(4, 4, 128, "bf16")
+    cache = B.PagedCache(layout, 1, 128, fmt=B.QP_CACHE_FP8_E4M3)
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(128, 4, 128)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    batch = B.PagedBatch(i32([[0]]), i32([128]), i32([0, 128]), 128)
+    B.paged_append(layout, cache, batch, bits.to(DEV), bits.flip(0).contiguous().to(DEV), torch.arange(128, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    want = torch.tensor([B.lib().qp_e4m3_from_bf16(x) for x in range(65536)], dtype=torch.uint8).view(128, 4, 128)
+    assert torch.equal(cache.k[0].view(torch.uint8).cpu(), want.transpose(0, 1))
+    assert torch.equal(cache.v[0].view(torch.uint8).cpu(), want.flip(0).transpose(0, 1))
+
+
 def test_append_of_rows_that_are_e4m3_already():
     sc = Scene(L72, 64, [200, 130], [200, 65], seed=2, fp8=True)
     g = torch.Generator().manual_seed(3)

@@ -250,8 +250,6 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, 
       eq += key[c] == thr;
     }
   };
-  // the comparisons are cheaper to make again than to keep
-  auto forget = [](uint4& k) { asm volatile("" : "+v"(k.x), "+v"(k.y), "+v"(k.z), "+v"(k.w)); };
   uint32_t gt = 0, eq = 0;  // before the block
   auto block = [&](const uint4& k, int u, int r) {
     uint32_t gt_w = gt, eq_w = eq;
@@ -267,13 +265,55 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, 
   };
   if constexpr (HELD) {
 #pragma unroll
-    for (int u = 0; u < EV_HELD; ++u)
+    for (int u = 0; u < EV_HELD; ++u) {
       if (u < used) tally(held[u], u);
+      else if (lane == 0) run_gt[u][wave] = run_eq[u][wave] = 0;
+    }
     __syncthreads();
+    // the first wavefront turns the runs' counts, in order, into what lies before each
+    static_assert(EV_HELD * SEL_WAVES == 3 * 64, "three runs per lane");
+    if (wave == 0) {
+      uint32_t* const g = &run_gt[0][0] + 3 * lane;
+      uint32_t* const q = &run_eq[0][0] + 3 * lane;
+      const uint32_t g0 = g[0], g1 = g[1], g2 = g[2], q0 = q[0], q1 = q[1], q2 = q[2];
+      uint32_t gs = g0 + g1 + g2, qs = q0 + q1 + q2;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = __shfl_up(gs, o, 64), y = __shfl_up(qs, o, 64);
+        if (lane >= o) gs += x, qs += y;
+      }
+      if (lane == 63) red[0][0] = qs;
+      gs -= g0 + g1 + g2;
+      qs -= q0 + q1 + q2;
+      g[0] = gs, g[1] = gs + g0, g[2] = gs + g0 + g1;
+      q[0] = qs, q[1] = qs + q0, q[2] = qs + q0 + q1;
+    }
+    __syncthreads();
+    // Nearly always all keys equal to the threshold stay, or none: then nobody asks which of them.
+    const bool alike = need == 0 || red[0][0] == need;
 #pragma unroll
     for (int u = 0; u < EV_HELD; ++u) {
-      forget(held[u]);
-      if (u < used) block(held[u], u, u);
+      if (u >= used) break;
+      const uint32_t gt_run = run_gt[u][wave], eq_run = run_eq[u][wave];
+      const int j = u * EV_BLOCK + 4 * tid;
+      if (!alike) {
+        emit(held[u], j, gt_run, eq_run);
+        continue;
+      }
+      const uint32_t key[4] = {held[u].x, held[u].y, held[u].z, held[u].w};
+      uint32_t slot = gt_run + (need > 0 ? eq_run : 0u);
+      const uint32_t least = need > 0 ? thr : thr + 1;  // thr < EV_STAYS; key 0 never stays
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const unsigned long long m = __ballot(key[c] >= least);
+        slot = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, slot));
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bool stay = key[c] >= least;
+        if (stay && slot < (uint32_t)e.keep) kept[slot] = j + c;
+        slot += stay;
+      }
     }
   } else {
     for (int u = 0; u < used; ++u) {

@@ -81,8 +81,8 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
  * sees no entry (its sequence is empty, or longer than its table) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (few rows: to two bf16 terms),
  * never in the sums behind lse. What a row does not see does not reach its result, infinities and NaN included.
- *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to key chunks whose partial
- *     results (f32) lie there until a second launch merges them; without it (or with less) chunks are fewer and longer. */
+ *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups
+ *     whose partial results (f32) lie there until a second launch merges them; without it (or with less) to fewer. */
 qp_status qp_paged_attend(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, const void* q,
                           void* out, float* lse_or_null, void* workspace, size_t workspace_bytes, void* hip_stream);
 
@@ -106,10 +106,12 @@ qp_status qp_paged_evict(const qp_layout* layout, const qp_paged_cache* cache, c
                          int32_t n_first, int32_t n_last, const int32_t* to_table, int32_t to_pages, int32_t* to_len,
                          int32_t* kept_or_null, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* How qp_paged_attend would lay out a call (host arithmetic only): row tiles of a sequence and KV head, key chunks of max_len
- * entries (1: one launch, no scratch), entries per chunk, scratch taken. */
+/* How qp_paged_attend would lay out a call (host arithmetic only). Few rows: `shares` workgroups of every KV head divide the entries
+ * of all sequences evenly among them (0: a workgroup per sequence, head and row tile, no scratch). Chunks over bf16 heads of 128:
+ * key_chunks of chunk_entries of every sequence (1: no scratch). */
 typedef struct {
   int32_t rows_per_tile; /* stacked rows (tokens x query heads of a KV head) of one workgroup: 16, 32 or 256 */
+  int32_t shares;
   int32_t key_chunks;
   int32_t chunk_entries;
   int32_t workgroups;

@@ -66,7 +66,7 @@ class qp_paged_batch(ctypes.Structure):
 
 
 class qp_paged_plan_info(ctypes.Structure):
-    _fields_ = [("rows_per_tile", ctypes.c_int32), ("key_chunks", ctypes.c_int32), ("chunk_entries", ctypes.c_int32),
+    _fields_ = [("rows_per_tile", ctypes.c_int32), ("shares", ctypes.c_int32), ("key_chunks", ctypes.c_int32), ("chunk_entries", ctypes.c_int32),
                 ("workgroups", ctypes.c_int32), ("scratch_bytes", ctypes.c_size_t)]
 
 

@@ -66,7 +66,8 @@ bool launch_paged_append(const PagedArgs& a, const PagedAppend& src, int dtype, 
 
 struct PagedPlan {
   int tile_rows, tiles;    // stacked rows per workgroup, tiles of max_new tokens
-  int chunks, chunk_keys;
+  int chunks, chunk_keys;  // tile kernel: key chunks of a sequence
+  int shares;              // few rows: workgroups of a KV head among which all entries are dealt, 0: one per tile
   long long workgroups;
   size_t scratch_bytes;
 };

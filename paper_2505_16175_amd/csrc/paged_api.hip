@@ -172,6 +172,7 @@ qp_status qp_paged_plan(const qp_layout* L, const qp_paged_cache* cache, const q
   memset(out, 0, sizeof(*out));
   if (p.workgroups > 0x7fffffffll) return QP_ERR_UNSUPPORTED;
   out->rows_per_tile = p.tile_rows;
+  out->shares = p.shares;
   out->key_chunks = p.chunks;
   out->chunk_entries = p.chunk_keys;
   out->workgroups = (int32_t)p.workgroups;

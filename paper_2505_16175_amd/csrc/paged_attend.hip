@@ -6,9 +6,9 @@
 // paged_rows_kernel: few stacked rows (tokens x query heads of a KV head; decoding, drafted tokens) against a long axis, and
 // other layouts. What
 // bounds it is HBM: K and V are read once and nothing is reused, and the products take a tenth of that time. So there is no LDS
-// tile and no barrier in its loop: a workgroup takes a chunk of a sequence's entries for one KV head, its four wavefronts take
+// tile and no barrier in its loop: a workgroup takes an equal share of the batch's entries for one KV head, its four wavefronts take
 // blocks of 32 keys (16 of f32) in turn, each straight into registers (paged_rows.h) while the block before it is computed;
-// chunks' partial results are merged by a second launch.
+// partial results of sequences that shares cut are merged by a second launch.
 //   S^T = K Q^T, P^T = exp2(c S^T - m), O^T += V^T P^T; a lane holds one row and 8 of the block's keys. The reference m of a row
 //   moves only when a logit exceeds it by 2^8, so that most blocks exchange nothing between lanes. Numerators are rounded to bf16
 //   twice (their value, and what that lost), so that 16-bit results differ from exact ones by their own rounding: the second
@@ -27,43 +27,37 @@ struct PagedOut {
   const void* q;   // [n_rows][h_q][d]
   void* out;
   float* lse;      // [h_q][n_rows] or nullptr
-  float* part_o;   // [chunks][n_rows * h_q][d], chunks > 1
-  float* part_lse; // [chunks][n_rows * h_q], log2 units
+  float* part_o;   // partial results: tile kernel [chunks][n_rows * h_q][d]; shares [h_kv][shares + units][rows of a tile][d]
+  float* part_lse; // the same without d, log2 units
   int tiles, chunks, chunk_keys;
+  int shares;      // workgroups of a KV head among which the batch's blocks are dealt; 0: one for each unit, or the tile kernel
+  int tile_rows;
+  int2* info;      // [units]: first share of a unit and the shares that have blocks of it
 };
 
-// Two workgroups per compute unit where two blocks' rows fit half of the registers.
+// Two workgroups per compute unit where a block's registers leave room for it. Of bf16 heads of 128 one has the registers to itself:
+// squeezed into half of them its results and addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26.
 template <typename E, int D, int RT>
-constexpr int pr_waves() { return D == 64 || (sizeof(E) < 4 && RT == 1) || sizeof(E) == 1 ? 2 : 1; }
+constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 
+// Where the workgroups' results meet.
+template <int D, int ROWS>
+struct RowsLds {
+  int pages[PR_LIST];
+  float m[PR_NW][ROWS], l[PR_NW][ROWS];
+  __attribute__((aligned(16))) float slab[PR_NW][ROWS][D + 4];
+};
+
+// Keys [k_begin, k_end) of one unit, a row tile of sequence s; slot: where its partial result goes, -1: it is the whole, and the output.
 template <typename E, int D, int RT>
-__global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
+__device__ __forceinline__ void rows_unit(const PagedArgs& a, const PagedOut& o, RowsLds<D, 16 * RT>& lds, const PagedSeq& q, int s, int h,
+                                          int row0, int n_rows, int k_begin, int k_end, long long slot) {
   using L = RowsLayout<E, D>;
   using Block = RowsBlock<E, D>;
-  constexpr int NE = L::NE, ROWS = 16 * RT, LD = D + 4;
-  __shared__ int pages[PR_LIST];
-  __shared__ float sm_m[PR_NW][ROWS], sm_l[PR_NW][ROWS];
-  __shared__ __attribute__((aligned(16))) float slab[PR_NW][ROWS][LD];
+  constexpr int NE = L::NE, ROWS = 16 * RT;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // workgroup -> (chunk, sequence, row tile, head): one head's tiles of a chunk meet on few XCDs
-  int x = blockIdx.x;
-  const int h = x % a.h_kv;
-  x /= a.h_kv;
-  const int tile = x % o.tiles;
-  x /= o.tiles;
-  const int s = x % a.n_seqs, chunk = x / a.n_seqs;
-  const PagedSeq q = paged_seq_of(a, s);
   const int r_heads = a.h_q / a.h_kv;
-  const long long all_rows = (long long)q.n * r_heads;
-  const int row0 = tile * ROWS;
-  if (row0 >= all_rows) return;
-  if (chunk > 0 && (long long)chunk * o.chunk_keys >= q.len) return;  // chunk 0 always answers
-  const int n_rows = (int)(all_rows - row0 < ROWS ? all_rows - row0 : ROWS);
-  const int lim_max = q.base + (row0 + n_rows - 1) / r_heads;  // the last row sees most
-  const int k_begin = chunk * o.chunk_keys;
-  const int k_end = min(min(q.len, lim_max + 1), o.chunk_keys < q.len - k_begin ? k_begin + o.chunk_keys : q.len);
-
   RowsWave<E, D, RT> rows;
   rows.init(a, q, o.q, h, row0, n_rows);
   const float c2 = a.scale_log2;
@@ -71,7 +65,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
 
   auto load = [&](Block& b, int key0) {
     rows.load(b, a, h, key0, k_end,
-              [&](int key) { return __builtin_amdgcn_readfirstlane(pages[(key >> a.page_shift) - (seg >> a.page_shift)]); });
+              [&](int key) { return __builtin_amdgcn_readfirstlane(lds.pages[(key >> a.page_shift) - (seg >> a.page_shift)]); });
   };
   auto compute = [&](Block& b, int key0) { rows.compute(b, key0, k_end, c2); };
 
@@ -79,7 +73,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
     const int seg_end = min(k_end, k_end - seg > PR_SEGMENT ? seg + PR_SEGMENT : k_end);
     const int first = seg >> a.page_shift, count = ((seg_end - 1) >> a.page_shift) - first + 1;
     __syncthreads();  // the last segment's list has been read
-    for (int i = tid; i < count; i += PR_NW * 64) pages[i] = a.table[(size_t)s * a.table_pages + first + i];
+    for (int i = tid; i < count; i += PR_NW * 64) lds.pages[i] = a.table[(size_t)s * a.table_pages + first + i];
     __syncthreads();
     Block b0, b1;
     int key = seg + wave * L::BK;
@@ -101,10 +95,10 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
   for (int t = 0; t < RT; ++t) {
     const float z = rows.denominator(t);
     if (g == 0) {
-      sm_m[wave][16 * t + l16] = rows.m[t];
-      sm_l[wave][16 * t + l16] = z;
+      lds.m[wave][16 * t + l16] = rows.m[t];
+      lds.l[wave][16 * t + l16] = z;
     }
-    float* const to = &slab[wave][16 * t + l16][4 * NE * g];
+    float* const to = &lds.slab[wave][16 * t + l16][4 * NE * g];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -112,19 +106,18 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
         *(float4*)(to + NE * r + e) = make_float4(rows.acc[t][e][r], rows.acc[t][e + 1][r], rows.acc[t][e + 2][r], rows.acc[t][e + 3][r]);
   }
   __syncthreads();
-  const size_t total = (size_t)a.n_rows * a.h_q;
   for (int z = tid; z < n_rows * (D / 4); z += PR_NW * 64) {
     const int r = z / (D / 4), d = (z - r * (D / 4)) * 4;
-    float big = sm_m[0][r];
+    float big = lds.m[0][r];
 #pragma unroll
-    for (int w = 1; w < PR_NW; ++w) big = fmaxf(big, sm_m[w][r]);
+    for (int w = 1; w < PR_NW; ++w) big = fmaxf(big, lds.m[w][r]);
     float den = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < PR_NW; ++w) {
-      const float wgt = __builtin_amdgcn_exp2f(sm_m[w][r] - big);
-      const float4 v = *(const float4*)&slab[w][r][d];
-      den = fmaf(wgt, sm_l[w][r], den);
+      const float wgt = __builtin_amdgcn_exp2f(lds.m[w][r] - big);
+      const float4 v = *(const float4*)&lds.slab[w][r][d];
+      den = fmaf(wgt, lds.l[w][r], den);
       sum.x = fmaf(wgt, v.x, sum.x);
       sum.y = fmaf(wgt, v.y, sum.y);
       sum.z = fmaf(wgt, v.z, sum.z);
@@ -137,8 +130,8 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
     const float lse2 = none ? -INFINITY : big + log2f(den);
     const int row = row0 + r, i = row / r_heads, qh = h * r_heads + (row - i * r_heads);
     const size_t at = (size_t)(q.row0 + i) * a.h_q + qh;
-    if (o.chunks > 1) {
-      const size_t p = (size_t)chunk * total + at;
+    if (slot >= 0) {
+      const size_t p = (size_t)slot * ROWS + r;
       *(float4*)(o.part_o + p * D + d) = sum;
       if (d == 0) o.part_lse[p] = lse2;
     } else {
@@ -149,6 +142,121 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows
                        (uint32_t)f32_to_bf16_rne(sum.z) | ((uint32_t)f32_to_bf16_rne(sum.w) << 16));
       if (o.lse != nullptr && d == 0) o.lse[(size_t)qh * a.n_rows + q.row0 + i] = lse2 * 0.6931471805599453f;
     }
+  }
+}
+
+// A unit is a row tile of a sequence that has rows; its blocks are the PR_NW wavefronts' keys up to the last that a row sees.
+constexpr int PR_UNITS = 2048;  // units whose blocks a workgroup adds up
+template <int RT>
+__device__ __forceinline__ int unit_blocks(const PagedArgs& a, const PagedSeq& q, int tile, int step) {
+  const int r_heads = a.h_q / a.h_kv;
+  const long long all_rows = (long long)q.n * r_heads, row0 = (long long)tile * (16 * RT);
+  if (row0 >= all_rows) return 0;
+  const int last = (int)((min(row0 + 16 * RT, all_rows) - 1) / r_heads);
+  return max(1, (min(q.len, q.base + last + 1) + step - 1) / step);  // one at least: a unit that sees nothing has results too
+}
+
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
+  constexpr int ROWS = 16 * RT, STEP = PR_NW * RowsLayout<E, D>::BK;
+  __shared__ RowsLds<D, ROWS> lds;
+  const int tid = threadIdx.x;
+  const int r_heads = a.h_q / a.h_kv;
+  const int h = blockIdx.x % a.h_kv;
+  const bool shared = o.shares > 0;  // else the workgroup has a unit, and what follows one round of the loop
+  // The blocks of all units, one after the other, in `shares` equal parts: lengths that differ, which only the device knows, leave
+  // nobody waiting. Every workgroup adds the units up for itself; of up to 64 every wavefront does, without a barrier (all write the
+  // same to LDS), and keeps what the device arrays say about their sequences.
+  __shared__ int before[PR_UNITS + 1], wave_sum[PR_NW];
+  __shared__ PagedSeq seqs[64];
+  const int lane = tid & 63, wave = tid >> 6;
+  const int share = blockIdx.x / a.h_kv, units = a.n_seqs * o.tiles;
+  const bool few = shared && units <= 64 && units > 1;
+  int begin = 0, end = 1, u = share, all = 0, per = 0, more = 0;
+  auto scan = [&](int sum) {
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const int y = __shfl_up(sum, x, 64);
+      if (lane >= x) sum += y;
+    }
+    return sum;
+  };
+  if (few) {
+    int n = 0;
+    if (lane < units) {
+      const PagedSeq q = paged_seq_of(a, lane / o.tiles);
+      n = unit_blocks<RT>(a, q, lane % o.tiles, STEP);
+      seqs[lane] = q;
+    }
+    const int sum = scan(n);
+    if (lane < units) before[lane] = sum - n;
+    if (lane == units - 1) before[units] = sum;
+    all = __builtin_amdgcn_readlane(sum, units - 1);
+  } else if (shared && units == 1) {  // one answer: nothing to add up
+    all = unit_blocks<RT>(a, paged_seq_of(a, 0), 0, STEP);
+  } else if (shared) {
+    for (int u0 = 0; u0 < units; u0 += PR_NW * 64) {
+      const int v = u0 + tid;
+      const int n = v < units ? unit_blocks<RT>(a, paged_seq_of(a, v / o.tiles), v % o.tiles, STEP) : 0;
+      const int sum = scan(n);
+      if (lane == 63) wave_sum[wave] = sum;
+      __syncthreads();
+      int at = all;
+#pragma unroll
+      for (int w = 0; w < PR_NW; ++w) {
+        if (w < wave) at += wave_sum[w];
+        all += wave_sum[w];
+      }
+      if (v < units) before[v] = at + sum - n;
+      __syncthreads();  // wave_sum has been read
+    }
+    if (tid == 0) before[units] = all;
+    __syncthreads();
+    all = __builtin_amdgcn_readfirstlane(all);  // the same in all lanes, which the compiler cannot see, nor of what comes from LDS
+  }
+  if (shared) {
+    const int shares = min(o.shares, all);  // each has a block at least
+    if (share >= shares) return;
+    per = all / shares;
+    more = all - per * shares;  // the first ones have one more
+    begin = share * per + min(share, more);
+    end = begin + per + (share < more);
+    // the unit with block `begin`: the last that starts there or before (units without rows have no blocks)
+    u = 0;
+    for (int step = units == 1 ? 0 : units > 64 ? PR_UNITS / 2 : 32; step > 0; step >>= 1)
+      if (u + step <= units && __builtin_amdgcn_readfirstlane(before[u + step]) <= begin) u += step;
+  }
+  auto share_of = [&](int block) {
+    const int longer = more * (per + 1);
+    return block < longer ? block / (per + 1) : more + (block - longer) / per;
+  };
+  for (int at = begin; at < end; ++u) {
+    const bool listed = shared && units > 1;
+    const int from = listed ? __builtin_amdgcn_readfirstlane(before[u]) : 0, to = listed ? __builtin_amdgcn_readfirstlane(before[u + 1]) : shared ? all : 1;
+    if (from == to) continue;
+    const int s = u / o.tiles, row0 = (u - s * o.tiles) * ROWS;
+    PagedSeq q;
+    if (few) {
+      q.len = __builtin_amdgcn_readfirstlane(seqs[u].len);
+      q.row0 = __builtin_amdgcn_readfirstlane(seqs[u].row0);
+      q.n = __builtin_amdgcn_readfirstlane(seqs[u].n);
+      q.base = __builtin_amdgcn_readfirstlane(seqs[u].base);
+    } else {
+      q = paged_seq_of(a, s);
+    }
+    const int n_rows = (int)min((long long)q.n * r_heads - row0, (long long)ROWS);
+    if (n_rows <= 0) return;  // not shared: a tile without rows
+    const int stop = min(to, end);
+    const int k_end = min(stop == to ? 0x7fffffff : (stop - from) * STEP, min(q.len, q.base + (row0 + n_rows - 1) / r_heads + 1));
+    const bool whole = at == from && stop == to;
+    if (shared && h == 0 && at == from && tid == 0) {
+      const int first = share_of(from);
+      o.info[u] = make_int2(first, share_of(to - 1) - first + 1);
+    }
+    __syncthreads();  // the last unit's results have been read
+    rows_unit<E, D, RT>(a, o, lds, q, s, h, row0, n_rows, (at - from) * STEP, k_end,
+                        whole ? -1ll : (long long)h * (o.shares + units) + share + u);
+    at = stop;
   }
 }
 
@@ -168,8 +276,19 @@ __global__ __launch_bounds__((W == 1 ? PM_WAVES : W) * 64) void paged_merge_kern
   const long long item = (long long)(blockIdx.x - s * per_seq) * ROWS + (W == 1 ? wave : 0);
   const int i = (int)(item / a.h_q), qh = (int)(item - (long long)i * a.h_q);
   if (i >= q.n) return;  // with W > 1: the whole workgroup
-  const int n = q.len == 0 ? 1 : (q.len - 1) / o.chunk_keys + 1;  // chunks that answered
-  const size_t total = (size_t)a.n_rows * a.h_q, at = (size_t)(q.row0 + i) * a.h_q + qh;
+  const size_t at = (size_t)(q.row0 + i) * a.h_q + qh;
+  int n = q.len == 0 ? 1 : (q.len - 1) / o.chunk_keys + 1;  // chunks that answered
+  size_t first = at, stride = (size_t)a.n_rows * a.h_q;     // their rows among the partial results
+  if (o.shares > 0) {
+    const int r_heads = a.h_q / a.h_kv, h = qh / r_heads;
+    const long long row = (long long)i * r_heads + (qh - h * r_heads);
+    const int tile = (int)(row / o.tile_rows), u = s * o.tiles + tile;
+    const int2 info = o.info[u];
+    n = info.y;
+    if (n <= 1) return;  // one workgroup had the whole unit and wrote the output
+    first = ((size_t)h * (o.shares + a.n_seqs * o.tiles) + info.x + u) * o.tile_rows + (size_t)(row - (long long)tile * o.tile_rows);
+    stride = o.tile_rows;
+  }
   constexpr int B = 8;
   float m = PR_NONE, den = 0.f, sum[PER];
 #pragma unroll
@@ -178,7 +297,7 @@ __global__ __launch_bounds__((W == 1 ? PM_WAVES : W) * 64) void paged_merge_kern
     float ls[B], po[B][PER];
 #pragma unroll
     for (int u = 0; u < B; ++u) {
-      const size_t p = (size_t)min(c0 + u, n - 1) * total + at;
+      const size_t p = first + (size_t)min(c0 + u, n - 1) * stride;
       ls[u] = o.part_lse[p];
 #pragma unroll
       for (int e = 0; e < PER; ++e) po[u][e] = o.part_o[p * D + PER * lane + e];
@@ -234,11 +353,13 @@ __global__ __launch_bounds__((W == 1 ? PM_WAVES : W) * 64) void paged_merge_kern
   if (o.lse != nullptr && lane == 0)
     o.lse[(size_t)qh * a.n_rows + q.row0 + i] = none ? -INFINITY : (m + log2f(den)) * 0.6931471805599453f;
 }
-// Eight wavefronts share a row of more than 16 chunks.
+// Eight wavefronts share a row of more than 16 chunks (of shares: so many per unit where all are as long as may be).
 constexpr int PM_SHARE = 8;
-static int merge_rows(int chunks) { return chunks > 16 ? 1 : PM_WAVES; }
-static long long merge_blocks(const PagedArgs& a, int chunks) {
-  const int rows = merge_rows(chunks);
+static int merge_rows(const PagedArgs& a, const PagedPlan& p) {
+  return (p.shares > 0 ? p.shares / ((long long)a.n_seqs * p.tiles) : p.chunks) > 16 ? 1 : PM_WAVES;
+}
+static long long merge_blocks(const PagedArgs& a, const PagedPlan& p) {
+  const int rows = merge_rows(a, p);
   return (((long long)a.max_new * a.h_q + rows - 1) / rows) * a.n_seqs;
 }
 
@@ -249,31 +370,44 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   PagedPlan p{};
   const long long rows = (long long)a.max_new * (a.h_q / a.h_kv);
   const bool tiled = dtype == QP_BF16 && d == 128 && rows > PT_FROM_ROWS && rows <= PT_MOST_ROWS;
-  const int step = tiled ? 64 : PR_NW * (dtype == QP_F32 ? 16 : 32);  // entries of a chunk are a multiple of it
   p.tile_rows = tiled ? PT_ROWS : rows <= 16 ? 16 : 32;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
-  const long long units = (long long)a.n_seqs * a.h_kv * p.tiles;
-  // Rows: one workgroup per compute unit, two over 8-bit pools, of at least two blocks per wavefront. us by workgroups per compute
-  // unit 1 / 2 / 4: one token of the 7B heads over 46,125 entries 25.0 / 27.6 / 30.1, of 32 sequences over up to 9,840 84.8 / 89.8 /
-  // 93.2; up to four of the 72B heads of 16 sequences over 8-bit pages of up to 32,768 251 / 180 / 187.
-  // Tiles, one workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys (four questions of up to
-  // 300 tokens over up to 46,125 entries, one round 544, two 580, three 555, four 506, six 531).
-  const int rounds = tiled ? 4 : a.fp8 ? 2 : 1;
-  const long long want = std::max<long long>(1, ((long long)rounds * device_cu_count() + units - 1) / units);
-  const long long least = tiled ? 16 * 64 : 2 * step;
-  long long keys = std::max<long long>(((a.max_len + want - 1) / want + step - 1) / step * step, least);
+  p.chunks = 1;
+  p.chunk_keys = a.max_len;
+  scratch_bytes = std::min(scratch_bytes, PAGED_ATTEND_SCRATCH);
+  const long long units = (long long)a.n_seqs * p.tiles, cus = device_cu_count();
+  if (!tiled) {
+    // One workgroup per compute unit, two over 8-bit pools, whose blocks are longer chains over half the bytes, as long as each has
+    // a block. us, equal shares of all entries / equal chunks of the longest sequence (1, 2 and 4 workgroups per compute unit): up to
+    // four tokens of 16 sequences of the 72B heads over 8-bit pages of up to 32,768 entries 163 / 251, 180, 187; one token of 32
+    // sequences of the 7B heads over up to 9,840 79.0 / 84.8, 89.8, 93.2, of one over 46,125 26.0 / 25.0, 27.6, 30.1.
+    const int step = PR_NW * (dtype == QP_F32 ? 16 : 32);
+    const long long blocks = units * (((long long)a.max_len + step - 1) / step);
+    p.workgroups = units * a.h_kv;
+    long long shares = std::min(std::max<long long>(1, (a.fp8 ? 2 : 1) * cus / a.h_kv), blocks);
+    if (units > PR_UNITS || blocks > 0x7fffffff || a.max_len <= 2 * step) return p;
+    const size_t per_share = (size_t)a.h_kv * p.tile_rows * (d + 1) * sizeof(float), info = (size_t)units * sizeof(int2);
+    shares = std::min(shares, scratch_bytes < info ? 0ll : (long long)((scratch_bytes - info) / per_share) - units);
+    if (shares < 2) return p;
+    p.shares = (int)shares;
+    p.workgroups = shares * a.h_kv;
+    p.scratch_bytes = info + (size_t)(shares + units) * per_share;
+    return p;
+  }
+  // One workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys (four questions of up to 300
+  // tokens over up to 46,125 entries: one round 544 us, two 580, three 555, four 506, six 531).
+  const long long want = std::max<long long>(1, (4 * cus + units * a.h_kv - 1) / (units * a.h_kv));
+  long long keys = std::max<long long>(((a.max_len + want - 1) / want + 63) / 64 * 64, 16 * 64);
   const size_t per_chunk = (size_t)a.n_rows * a.h_q * (d + 1) * sizeof(float);
   long long chunks = (a.max_len + keys - 1) / keys;
-  const long long fit = (long long)(std::min(scratch_bytes, PAGED_ATTEND_SCRATCH) / per_chunk);
+  const long long fit = (long long)(scratch_bytes / per_chunk);
   if (chunks > fit) {
     chunks = fit >= 2 ? fit : 1;
-    keys = ((a.max_len + chunks - 1) / chunks + step - 1) / step * step;
+    keys = ((a.max_len + chunks - 1) / chunks + 63) / 64 * 64;
     chunks = (a.max_len + keys - 1) / keys;
   }
-  p.chunks = (int)std::max<long long>(chunks, 1);
-  p.chunk_keys = (int)std::min<long long>(keys, 0x40000000);
-  p.workgroups = tiled ? paged_tile_blocks(a, p) : units * p.chunks;
-  p.scratch_bytes = p.chunks > 1 ? per_chunk * p.chunks : 0;
+  if (chunks > 1) p.chunks = (int)chunks, p.chunk_keys = (int)keys, p.scratch_bytes = per_chunk * p.chunks;
+  p.workgroups = paged_tile_blocks(a, p);
   return p;
 }
 
@@ -283,9 +417,9 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
   if (p.tile_rows == PT_ROWS) launch_paged_tiles(a, p, o.q, o.out, o.lse, o.part_o, o.part_lse, s);
   else if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1>), grid, block, 0, s, a, o);
   else hipLaunchKernelGGL((paged_rows_kernel<E, D, 2>), grid, block, 0, s, a, o);
-  if (p.chunks > 1) {
-    const dim3 merge((unsigned)merge_blocks(a, p.chunks));
-    if (merge_rows(p.chunks) == 1) hipLaunchKernelGGL((paged_merge_kernel<T, D, PM_SHARE>), merge, dim3(PM_SHARE * 64), 0, s, a, o);
+  if (p.chunks > 1 || p.shares > 0) {
+    const dim3 merge((unsigned)merge_blocks(a, p));
+    if (merge_rows(a, p) == 1) hipLaunchKernelGGL((paged_merge_kernel<T, D, PM_SHARE>), merge, dim3(PM_SHARE * 64), 0, s, a, o);
     else hipLaunchKernelGGL((paged_merge_kernel<T, D, 1>), merge, dim3(PM_WAVES * 64), 0, s, a, o);
   }
   return true;
@@ -294,12 +428,16 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
 bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, void* out, float* lse, void* scratch,
                          size_t scratch_bytes, hipStream_t s) {
   const PagedPlan p = plan_paged_attend(a, dtype, d, scratch != nullptr ? scratch_bytes : 0);
-  if (p.workgroups * (p.tile_rows == PT_ROWS ? 512 : PR_NW * 64) > PAGED_MAX_THREADS || merge_blocks(a, p.chunks) * PM_SHARE * 64 > PAGED_MAX_THREADS) return false;
+  if (p.workgroups * (p.tile_rows == PT_ROWS ? 512 : PR_NW * 64) > PAGED_MAX_THREADS || merge_blocks(a, p) * PM_SHARE * 64 > PAGED_MAX_THREADS)
+    return false;
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;
+  o.shares = p.shares, o.tile_rows = p.tile_rows;
+  const size_t part_rows = p.shares > 0 ? (size_t)(p.shares + a.n_seqs * p.tiles) * a.h_kv * p.tile_rows : (size_t)p.chunks * a.n_rows * a.h_q;
   o.part_o = (float*)scratch;
-  o.part_lse = o.part_o + (size_t)p.chunks * a.n_rows * a.h_q * d;
+  o.part_lse = o.part_o + part_rows * d;
+  o.info = (int2*)(o.part_lse + part_rows);  // part_rows is even
   if (dtype == QP_F32) return d == 64 ? attend_as<float, float, 64>(a, o, p, s) : attend_as<float, float, 128>(a, o, p, s);
   if (a.fp8) return attend_as<uint8_t, bf16_t, 128>(a, o, p, s);
   return d == 64 ? attend_as<bf16_t, bf16_t, 64>(a, o, p, s) : attend_as<bf16_t, bf16_t, 128>(a, o, p, s);

@@ -163,6 +163,21 @@ def NUMERATORS(sc):
     return 2.0 ** -8 if p["rows_per_tile"] == 256 else None
 
 
+@pytest.mark.parametrize("layout,n_seqs,most,new", [(L7, 3, 3000, 2), (TINY, 64, 400, 3), (L7, 70, 500, 1), (TINY, 300, 300, 5), (TINY, 2100, 20, 1), (BF64, 9, 900, 40)])
+def test_many_sequences_of_very_different_lengths(layout, n_seqs, most, new):
+    """The entries of a batch are dealt evenly to workgroups, whatever the sequences' lengths: some of them empty, some without rows."""
+    g = torch.Generator().manual_seed(n_seqs)
+    lens = [0 if i % 7 == 3 else max(1, int(most * float(torch.rand(1, generator=g)) ** 3)) for i in range(n_seqs)]
+    news = [0 if i % 5 == 2 else 1 + (i * new) % new if new == 1 else int(torch.randint(1, new + 1, (1,), generator=g)) for i in range(n_seqs)]
+    lens[-1] = most
+    sc = Scene(layout, 16, lens, news, seed=n_seqs)
+    shares = B.paged_plan(sc.layout, sc.cache, sc.batch, sc.ws.numel())["shares"]
+    assert (shares > 1) == (n_seqs <= 300)
+    for ws in ("full", None, sc.ws[: sc.ws.numel() // 2 // 256 * 256]):
+        out, lse = sc.attend(ws)
+        sc.check_attend(out, lse)
+
+
 @pytest.mark.parametrize("layout,fp8", [(TINY, False), (L7, False), (L7, True), (BF64, False)])
 def test_long_sequences_against_a_sample(layout, fp8):
     """A sequence over several page lists of a workgroup (8192 entries each) where scratch is missing."""

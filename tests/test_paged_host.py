@@ -105,7 +105,9 @@ def test_plans_cover_the_entries_and_fit_what_is_offered(layout):
                         assert B.lib().qp_paged_plan(ctypes.byref(L), ctypes.byref(c), ctypes.byref(b), offered, ctypes.byref(p)) == B.QP_OK
                         assert p.key_chunks >= 1 and p.scratch_bytes <= min(offered, ws)
                         assert (p.key_chunks - 1) * p.chunk_entries < max_len <= p.key_chunks * p.chunk_entries
-                        assert p.chunk_entries % 16 == 0
+                        assert p.key_chunks == 1 or p.chunk_entries % 64 == 0
+                        assert p.shares == 0 or p.rows_per_tile < 256 and p.key_chunks == 1 and p.workgroups == p.shares * layout[1]
+                        assert (p.scratch_bytes > 0) == (p.shares > 0 or p.key_chunks > 1)
     assert B.lib().qp_paged_plan(ctypes.byref(L), ctypes.byref(c), ctypes.byref(b), 0, None) == INV
     assert B.paged_workspace_bytes(L, 0, 1, 1, 1) == 0 and B.paged_workspace_bytes(L, 1, 1, 1, 0) == 0
     assert B.paged_workspace_bytes(L, 1, 1, 1, 1, -1) == 0

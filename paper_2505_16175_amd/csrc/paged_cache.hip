@@ -223,7 +223,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, 
   if (count < total) {
     thr = EV_STAYS - 1;        // only those that stay in any case
     if (count > stays)         // and the largest of the others, whose keys alone the search spreads over its buckets
-      select_threshold<false>(each, lo, hi, count - stays, lds, thr, need);
+      select_threshold<false>(each, each, lo, hi, count - stays, lds, thr, need);
   }
 
   // The list, in order: an entry above the threshold stays, one equal to it if fewer than `need` of those lie before it, and its

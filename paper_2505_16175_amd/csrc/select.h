@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t order_key(float s) {
 }
 
 struct SelectLds {
-  __attribute__((aligned(16))) uint32_t hist[SEL_NB];  // zero at entry, and again when the search returns
+  __attribute__((aligned(8))) uint32_t hist[SEL_NB];  // zero at entry, and again when the search returns
   uint32_t list[SEL_LIST];
   uint32_t wave_a[SEL_WAVES];
   uint32_t sel_bucket, sel_need, sel_count, sel_key, list_n;  // list_n: zero at entry
@@ -58,11 +58,12 @@ __device__ __forceinline__ EachKey<UNROLL, KeyAt> each_key(KeyAt key_at, int n) 
 }
 
 // thr: the rank-th largest of the keys that `each` hands to the workgroup's threads, as far as they are inside [lo, hi]
-// (1 <= rank <= their number); need: how many keys equal to it are among the first `rank` (>= 1). The workgroup has met at a
-// barrier behind what it wrote to `lds` and to the keys. FOLD: keys that share a bucket are counted together first (above); without
-// it a list of equal keys takes a few times longer and every other one less.
-template <bool FOLD = true, class Each>
-__device__ __forceinline__ void select_threshold(Each each, uint32_t lo, uint32_t hi, uint32_t rank, SelectLds& lds,
+// (1 <= rank <= their number); need: how many keys equal to it are among the first `rank` (>= 1). `each` brings whole wavefronts;
+// `scan` hands out the same keys and need not (the list's pass has no ballot: n rounded up to the wavefronts costs a short TopK
+// 0.7 us of 12). The workgroup has met at a barrier behind what it wrote to `lds` and to the keys. FOLD: keys that share a bucket
+// are counted together first (above); without it a list of equal keys takes a few times longer and every other one less.
+template <bool FOLD = true, class Each, class Scan>
+__device__ __forceinline__ void select_threshold(Each each, Scan scan, uint32_t lo, uint32_t hi, uint32_t rank, SelectLds& lds,
                                                  uint32_t& thr, uint32_t& need) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t span = hi - lo;          // keys still in play: lo <= key <= lo + span
@@ -124,7 +125,7 @@ __device__ __forceinline__ void select_threshold(Each each, uint32_t lo, uint32_
     if (sh == 0) break;  // buckets were single keys: T = lo, `need` of its copies survive
     if (count <= SEL_LIST) {
       // rank the bucket's keys directly
-      each([&](uint32_t key, bool in) {
+      scan([&](uint32_t key, bool in) {
         if (in && key - lo <= span) {
           const uint32_t p = atomicAdd(&lds.list_n, 1u);
           if (p < (uint32_t)SEL_LIST) lds.list[p] = key;  // always true: the bucket holds `count` keys
@@ -134,13 +135,7 @@ __device__ __forceinline__ void select_threshold(Each each, uint32_t lo, uint32_
       if (tid < (int)count) {
         const uint32_t x = lds.list[tid];
         uint32_t g = 0, e = 0;
-        uint32_t m = 0;
-        for (; m + 4 <= count; m += 4) {
-          const uint4 y = *(const uint4*)&lds.list[m];
-          g += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
-          e += (y.x == x) + (y.y == x) + (y.z == x) + (y.w == x);
-        }
-        for (; m < count; ++m) {
+        for (uint32_t m = 0; m < count; ++m) {
           const uint32_t y = lds.list[m];
           g += y > x;
           e += y == x;

@@ -116,7 +116,10 @@ __global__ __launch_bounds__(TOPK_THREADS) void topk_compact_kernel(TopkArgs a, 
   }
 
   uint32_t thr, need;
-  select_threshold(each_key([&](int j) { return keys[j]; }, n), lo, hi, (uint32_t)a.keep, lds, thr, need);
+  auto scan = [&](auto f) {
+    for (int j = tid; j < n; j += TOPK_THREADS) f(keys[j], true);
+  };
+  select_threshold(each_key([&](int j) { return keys[j]; }, n), scan, lo, hi, (uint32_t)a.keep, lds, thr, need);
   // thr: the k-th largest key; need: how many keys equal to it survive (>= 1)
 
   // this workgroup's slice of the tokens, and the (greater, equal) keys before it

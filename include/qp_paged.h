@@ -48,7 +48,8 @@ typedef struct {
 /* The sequences of a call. Sequence s has the entries 0 .. len[s] - 1, entry j in page page_table[s][j / page_tokens] at
  * j % page_tokens, and the new tokens of rows row_start[s] .. row_start[s + 1] - 1 (n_s of them, possibly none) of the call's
  * tensors, which are its LAST n_s entries: row i of s (from 0) is entry len[s] - n_s + i and sees the entries up to itself.
- * Rows before row_start[0] and from row_start[n_seqs] on belong to nobody and are left as they were. */
+ * Rows before row_start[0] and from row_start[n_seqs] on belong to nobody and are left as they were. A length beyond max_len or the
+ * end of the table counts as that end: the new tokens are then the last entries before it. */
 typedef struct {
   const int32_t* page_table; /* device, [n_seqs][table_pages]                                                  */
   const int32_t* len;        /* device, [n_seqs]: entries, the new ones included                               */
@@ -78,7 +79,7 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
                           int64_t pos_token_stride, int64_t pos_head_stride, qp_cache_format source_format, void* hip_stream);
 
 /* Attention of the new tokens: q, out [n_rows][H_q][d] (layout dtype), lse_or_null [H_q][n_rows] f32 (natural log). A row that
- * sees no entry (its sequence is empty, or longer than its table) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
+ * sees no entry (the sequence has fewer than its new rows, or none of its pages is there) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (few rows: to two bf16 terms),
  * never in the sums behind lse. What a row does not see does not reach its result, infinities and NaN included.
  *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups
@@ -97,7 +98,7 @@ qp_status qp_paged_weigh(const qp_layout* layout, const qp_paged_cache* cache, c
  * and the last n_last entries (n_first + n_last <= keep), and of the others those of the largest weight, equal weights (and
  * -0.0 == +0.0) by lower entry number; weights must not be NaN. They are stored in ascending order as entries 0, 1, ... of
  * the pages of to_table [n_seqs][to_pages], with their positions and weights, and to_len[s] becomes their number (the same for
- * all heads). The old pages are only read: the caller gives them back (or keeps them, where others share them). A sequence of at
+ * all heads; to_len may be the batch's len). The old pages are only read: the caller gives them back (or keeps them, where others share them). A sequence of at
  * most `keep` entries is copied whole, without its missing pages.
  *   kept_or_null [n_seqs][H_kv][keep]: their old entry numbers, -1 behind the last
  *   workspace: qp_paged_workspace_bytes(..., keep) bytes, needed

@@ -539,6 +539,7 @@ class PagedCache:
               for t, d, name in ((self.k, dt, "k"), (self.v, dt, "v"), (self.pos, torch.int32, "pos"))]
         at.append(None if self.weight is None else _dense(self.weight, torch.float32, rows, "weight", here))
         self.device_index = here
+        self.made_for = (layout.n_kv_heads, layout.head_dim, layout.dtype)
         self.c = qp_paged_cache(*at, n_pages, page_tokens, fmt)
         self.ref = ctypes.byref(self.c)
 
@@ -570,7 +571,9 @@ class PagedBatch:
         return self.ref
 
 
-def _same_gpu(cache, batch):
+def _same_gpu(layout, cache, batch):
+    if cache.made_for != (layout.n_kv_heads, layout.head_dim, layout.dtype):
+        raise ValueError("expected a cache of this layout's heads and dtype")
     here = _here()
     if cache.device_index != here or batch.device_index != here:
         raise ValueError("expected a cache and a batch of the current GPU")
@@ -594,7 +597,7 @@ def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
     """k, v [n_rows][H_kv][d] of any strides whose rows are runs of d elements (a flat cache's [H_kv][capacity][d] comes as
     k.transpose(0, 1)[:n]); pos int32 [n_rows], or [n_rows][H_kv] with a position per head. Rows of an 8-bit pool may be
     torch.float8_e4m3fn already."""
-    here = _same_gpu(cache, batch)
+    here = _same_gpu(layout, cache, batch)
     n, h_kv, d = batch.n_rows, layout.n_kv_heads, layout.head_dim
     shape, dt = (n, h_kv, d), k.dtype
     raw = dt is torch.float8_e4m3fn
@@ -618,7 +621,7 @@ def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
 
 def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None, workspace=None):
     """q, out [n_rows][H_q][d], lse float32 [H_q][n_rows]."""
-    here = _same_gpu(cache, batch)
+    here = _same_gpu(layout, cache, batch)
     dt, shape = _layout_dtype(layout), (batch.n_rows, layout.n_q_heads, layout.head_dim)
     wp, wb = _scratch(workspace, here)
     st = lib().qp_paged_attend(ctypes.byref(layout), cache.ref, batch.of(cache), _dense(q, dt, shape, "q", here),
@@ -629,7 +632,7 @@ def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None,
 
 def paged_weigh(layout, cache: PagedCache, batch: PagedBatch, q, lse, accumulate=True, workspace=None):
     """Adds to (or, accumulate=False, writes) cache.weight what the batch's rows of paged_attend's lse looked at."""
-    here = _same_gpu(cache, batch)
+    here = _same_gpu(layout, cache, batch)
     shape = (batch.n_rows, layout.n_q_heads, layout.head_dim)
     wp, wb = _scratch(workspace, here)
     st = lib().qp_paged_weigh(ctypes.byref(layout), cache.ref, batch.of(cache), _dense(q, _layout_dtype(layout), shape, "q", here),
@@ -639,7 +642,7 @@ def paged_weigh(layout, cache: PagedCache, batch: PagedBatch, q, lse, accumulate
 
 def paged_evict(layout, cache: PagedCache, batch: PagedBatch, keep, n_first, n_last, to_table, to_len, kept=None, workspace=None):
     """to_table int32 [n_seqs][pages], to_len int32 [n_seqs], kept int32 [n_seqs][H_kv][keep] or None."""
-    here = _same_gpu(cache, batch)
+    here = _same_gpu(layout, cache, batch)
     n_seqs = batch.n_seqs
     if to_table.dim() != 2 or to_table.shape[0] != n_seqs:
         raise ValueError("to_table: expected int32 [n_seqs][pages]")

@@ -428,8 +428,8 @@ static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p,
 bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, void* out, float* lse, void* scratch,
                          size_t scratch_bytes, hipStream_t s) {
   const PagedPlan p = plan_paged_attend(a, dtype, d, scratch != nullptr ? scratch_bytes : 0);
-  if (p.workgroups * (p.tile_rows == PT_ROWS ? 512 : PR_NW * 64) > PAGED_MAX_THREADS || merge_blocks(a, p) * PM_SHARE * 64 > PAGED_MAX_THREADS)
-    return false;
+  if (p.workgroups * (p.tile_rows == PT_ROWS ? 512 : PR_NW * 64) > PAGED_MAX_THREADS) return false;
+  if ((p.chunks > 1 || p.shares > 0) && merge_blocks(a, p) * PM_SHARE * 64 > PAGED_MAX_THREADS) return false;
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;

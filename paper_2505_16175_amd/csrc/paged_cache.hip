@@ -325,7 +325,6 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, 
     }
   }
   for (uint32_t x = count + tid; x < (uint32_t)e.keep; x += SEL_THREADS) kept[x] = -1;
-  if (h == 0 && tid == 0) e.to_len[s] = (int)count;
 }
 
 constexpr int EM_THREADS = 256;
@@ -342,6 +341,16 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move_kernel(PagedArgs a, Pag
   int from[EM_UNROLL];
 #pragma unroll
   for (int u = 0; u < EM_UNROLL; ++u) from[u] = x0 + u * ROWS < e.keep ? kept[x0 + u * ROWS] : -1;
+  if (h == 0 && sub == 0) {
+    // the new length is where the list ends: written here, since the heads' selections read the old one, which may be the same array
+#pragma unroll
+    for (int u = 0; u < EM_UNROLL; ++u) {
+      const int x = x0 + u * ROWS;
+      if (x >= e.keep) continue;
+      if (from[u] < 0 && (x == 0 || kept[x - 1] >= 0)) e.to_len[s] = x;
+      if (from[u] >= 0 && x == e.keep - 1) e.to_len[s] = e.keep;
+    }
+  }
   size_t src[EM_UNROLL], dst[EM_UNROLL];
 #pragma unroll
   for (int u = 0; u < EM_UNROLL; ++u) {

@@ -456,6 +456,33 @@ def test_evict_drops_what_has_no_destination():
     np.testing.assert_array_equal(got["k"][others], before["k"][others])
 
 
+@pytest.mark.parametrize("lens, keep", [([70, 5, 0, 300], 40), ([3], 64), ([50000, 12], 9)])
+def test_evict_writes_the_new_lengths_over_the_old(lens, keep):
+    """to_len the batch's own length: every head's selection still reads the old one."""
+    pages = -(-keep // 16)
+    sc = Scene(L72, 16, lens, [0] * len(lens), seed=keep, spare_pages=len(lens) * pages)
+    used = set(x for row in sc.table.tolist() for x in row)
+    free = [p for p in range(sc.cache.c.n_pages) if p not in used]
+    to = torch.tensor([[free.pop() for _ in range(pages)] for _ in lens], dtype=torch.int32, device=DEV)
+    kept = torch.empty(len(lens), sc.h_kv, keep, dtype=torch.int32, device=DEV)
+    want = P.evict(sc.pool(), sc.table.tolist(), lens, keep, 2, 3)
+    B.paged_evict(sc.layout, sc.cache, sc.batch, keep, 2, 3, to, sc.batch.length, kept, B.make_paged_workspace(sc.layout, sc.batch, keep, 16))
+    torch.cuda.synchronize()
+    assert sc.batch.length.tolist() == [min(n, keep) for n in lens]
+    for s in range(len(lens)):
+        for h in range(sc.h_kv):
+            w = want[s * sc.h_kv + h]
+            np.testing.assert_array_equal(kept[s, h].cpu().numpy()[:len(w)], w)
+
+
+def test_a_cache_of_another_layout_is_refused():
+    sc = Scene(L7, 16, [40], [1], seed=3)
+    other = B.make_layout(64, 8, 128, "bf16")
+    q = torch.zeros(sc.batch.n_rows, 64, 128, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        B.paged_attend(other, sc.cache, sc.batch, q, torch.empty_like(q))
+
+
 # ---- together ----
 
 def test_an_answer_goes_on_over_a_shared_video(seed=1):

@@ -222,8 +222,16 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, 
   uint32_t thr = 0, need = 0;  // every present entry stays
   if (count < total) {
     thr = EV_STAYS - 1;        // only those that stay in any case
-    if (count > stays)         // and the largest of the others, whose keys alone the search spreads over its buckets
-      select_threshold<false>(each, each, lo, hi, count - stays, lds, thr, need);
+    if (count > stays) {       // and the largest of the others, whose keys alone the search spreads over its buckets
+      bool many_low = true;
+      if constexpr (HELD) {    // one in eight of a sample
+        uint32_t low = 0;
+#pragma unroll
+        for (int u = 0; u < EV_HELD; ++u) low += (uint32_t)__popcll(__ballot(held[u].x == lo));
+        many_low = low >= 8u * (uint32_t)used;
+      }
+      select_threshold<false>(each, each, lo, hi, count - stays, lds, thr, need, many_low);
+    }
   }
 
   // The list, in order: an entry above the threshold stays, one equal to it if fewer than `need` of those lie before it, and its

@@ -61,10 +61,11 @@ __device__ __forceinline__ EachKey<UNROLL, KeyAt> each_key(KeyAt key_at, int n) 
 // (1 <= rank <= their number); need: how many keys equal to it are among the first `rank` (>= 1). `each` brings whole wavefronts;
 // `scan` hands out the same keys and need not (the list's pass has no ballot: n rounded up to the wavefronts costs a short TopK
 // 0.7 us of 12). The workgroup has met at a barrier behind what it wrote to `lds` and to the keys. FOLD: keys that share a bucket
-// are counted together first (above); without it a list of equal keys takes a few times longer and every other one less.
+// are counted together first (above). Without it that is done for the smallest keys alone, by wavefronts that have many of them
+// (`many_low`, the same in all lanes): entries that nothing looked at weigh 0.
 template <bool FOLD = true, class Each, class Scan>
 __device__ __forceinline__ void select_threshold(Each each, Scan scan, uint32_t lo, uint32_t hi, uint32_t rank, SelectLds& lds,
-                                                 uint32_t& thr, uint32_t& need) {
+                                                 uint32_t& thr, uint32_t& need, bool many_low = false) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t span = hi - lo;          // keys still in play: lo <= key <= lo + span
   need = rank;                      // of T among them, counted from the largest
@@ -72,7 +73,7 @@ __device__ __forceinline__ void select_threshold(Each each, Scan scan, uint32_t 
   for (int round = 0; round < SEL_MAX_ROUNDS; ++round) {
     const int bits = span ? 32 - __builtin_clz(span) : 0;
     const int sh = bits > SEL_BITS ? bits - SEL_BITS : 0;
-    each([&](uint32_t key, bool in) {
+    auto count_key = [&](uint32_t key, bool in) {
       const uint32_t off = key - lo;
       bool act = in && off <= span;  // a key below lo wraps to a large offset
       const uint32_t bin = off >> sh;
@@ -88,7 +89,18 @@ __device__ __forceinline__ void select_threshold(Each each, Scan scan, uint32_t 
         }
       }
       if (act) atomicAdd(&lds.hist[bin], 1u);
-    });
+    };
+    if (!FOLD && many_low) {
+      uint32_t low = 0;  // of this wavefront's keys in the first bucket
+      each([&](uint32_t key, bool in) {
+        const bool first = in && (key - lo) >> sh == 0;
+        low += (uint32_t)__popcll(__ballot(first));
+        count_key(key, in && !first);
+      });
+      if (lane == 0) atomicAdd(&lds.hist[0], low);
+    } else {
+      each(count_key);
+    }
     __syncthreads();
     // suffix sums over the buckets: this thread owns buckets 2 tid and 2 tid + 1 (and clears them for a next round)
     const uint2 hb = *(const uint2*)&lds.hist[2 * tid];

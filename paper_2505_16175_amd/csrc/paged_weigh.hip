@@ -1,14 +1,20 @@
 // The attention weight that the paged cache's entries received: w[j] (+)= sum over rows of exp2(c q.k_j - lse2), the column sums
 // of the softmax whose row statistics qp_paged_attend left. No atomics: an entry's sum is one lane's, from the first row to the last.
 //
-// paged_weigh_kernel: few rows (decoding, drafted tokens), and layouts without a tile kernel. A wavefront owns 64 entries (32 of
-// f32) of a KV head, whose keys stay in registers, and walks the sequence's rows 16 at a time: S = Q K^T leaves a lane with one
-// entry (column) and four rows. Bound by the keys' way from HBM, all of which is requested at once.
+// weigh_stream_kernel: few rows (decoding, drafted tokens). Queries and their statistics stay in registers, and a wavefront walks
+// blocks of 32 keys (16 of f32), the next one requested while it works on this: S = Q K^T leaves a lane with one entry (column) and
+// four rows. Bound by the keys' way from HBM: 3.7 TB/s (sums of a large array 4.0), where wavefronts that take 64 keys at once and
+// end reached 3.4 (54 us), and no more with fewer or more workgroups per compute unit.
+//
+// paged_weigh_kernel: chunks over layouts without a tile kernel. A wavefront owns 64 entries (32 of f32) of a KV head, whose keys stay
+// in registers, and walks the sequence's rows 16 at a time.
 //
 // weigh_tile_kernel: chunks over bf16 heads of 128. Four wavefronts own 64 entries each, keys in registers, and walk the rows 32 at a
 // time, which all of them read from LDS: tiles of queries go global -> LDS directly (XOR-swizzled 16-byte chunks), in a ring of four
 // slots, three ahead, one barrier each. Bound by the vector unit: a pair costs a multiply-add, an exponential at a quarter of the
-// rate and an add, 24 cycles per 64 pairs, beside the products' 16 on the matrix pipe.
+// rate and an add, 24 cycles per 64 pairs, beside the products' 16 on the matrix pipe. 500 tokens of the 7B heads over 46,125 entries
+// (one question): 98 us of exponentials, multiply-adds and adds at 2.4 GHz, 204 measured. Two wavefronts per SIMD that keep a second set of
+// scores, so that one tile's exponentials stand beside the next one's products, took 217-222, a barrier for every second tile the same.
 #include "paged_rows.h"
 
 #include <algorithm>
@@ -101,6 +107,114 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
     w[t] += __shfl_xor(w[t], 32, 64);
     const int key = key0 + 16 * t + l16;
     if (g == t && page[t] >= 0 && key < q.len) *to[t] = before + w[t];
+  }
+}
+
+// Entries of a workgroup: in pages of 16, at most one page number for each lane. One token of 32 sequences of the 7B heads over up to
+// 9,840 entries (187 MB of keys): 128 entries 65 us, 256 54.0, 384 50.0, 512 50.4, 1024 51.5.
+constexpr int WS_MOST = 512;
+template <typename E, int D, int RT>
+__global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_kernel(PagedArgs a, const void* __restrict__ qp_, const float* __restrict__ lse,
+                                                                               int accumulate, int entries) {
+  using L = RowsLayout<E, D>;
+  constexpr int STEP = PW_NW * L::BK;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int x = blockIdx.x;
+  const int h = x % a.h_kv;
+  x /= a.h_kv;
+  const int s = x % a.n_seqs;
+  const PagedSeq q = paged_seq_of(a, s);
+  const long long from = (long long)(x / a.n_seqs) * entries;
+  if (from >= q.len) return;
+  const int first = (int)from, end = min(q.len, first + entries);
+  const int r_heads = a.h_q / a.h_kv, mask = (1 << a.page_shift) - 1, page0 = first >> a.page_shift;
+  int list = -1;
+  if (page0 + lane <= (end - 1) >> a.page_shift) list = a.table[(size_t)s * a.table_pages + page0 + lane];
+
+  struct Block {
+    pr_u32x4 k[L::TILES][L::KL];
+    float* to;     // group t: the entry of tile t that this lane stores, nullptr: none
+    float before;
+  };
+  auto load = [&](Block& b, int key0) {
+    b.to = nullptr;
+    b.before = 0.f;
+#pragma unroll
+    for (int t = 0; t < L::TILES; ++t) {
+      const int key = key0 + 16 * t;
+      // a tile past the last entry takes the block's first page: read, never used
+      const int page = __builtin_amdgcn_readlane(list, ((key < end ? key : key0) >> a.page_shift) - page0);
+      const bool ok = paged_page_ok(page, a.n_pages);
+      const size_t row = paged_row(ok ? page : 0, h, key & mask, a.h_kv, a.page_shift);
+      rows_load_k<E, D>((const unsigned char*)a.k + row * L::ROWB, l16, g, b.k[t]);
+      if (g == t && ok && key + l16 < end) b.to = a.weight + row + l16;
+    }
+    if (accumulate && b.to != nullptr) b.before = *b.to;
+  };
+  const int n_rows = q.n * r_heads;  // 16 RT at most
+  pr_u32x4 qf[RT][L::QF];
+  float neg[RT][4];
+  int lim[RT][4];  // -1: a row that there is not, or that saw nothing
+  Block b0, b1;
+  int key = first + wave * L::BK;
+  if (key < end) load(b0, key);
+  bool all = true;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    if (n_rows > 0) {
+      const int row = min(16 * t + l16, n_rows - 1), i = row / r_heads;
+      const unsigned char* p = (const unsigned char*)qp_ + ((size_t)(q.row0 + i) * a.h_q + (size_t)h * r_heads + (row - i * r_heads)) * (D * L::QB);
+#pragma unroll
+      for (int u = 0; u < L::QF; ++u) qf[t][u] = *(const pr_u32x4*)(p + rows_q_byte<E, D>(u, g));
+    } else {
+#pragma unroll
+      for (int u = 0; u < L::QF; ++u) qf[t][u] = pr_u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      neg[t][r] = -INFINITY;
+      lim[t][r] = -1;
+      const int row = 16 * t + 4 * g + r;
+      if (row >= n_rows) continue;
+      const int i = row / r_heads;
+      const float z = lse[(size_t)(h * r_heads + row - i * r_heads) * a.n_rows + q.row0 + i];
+      neg[t][r] = -z * 1.4426950408889634f;
+      lim[t][r] = z != -INFINITY ? q.base + i : -1;
+      all = all && lim[t][r] >= end - 1;
+    }
+    all = all && 16 * (t + 1) <= n_rows;
+  }
+  const bool whole = __all(all);
+  const float c2 = a.scale_log2;
+  auto compute = [&](Block& b, int key0) {
+    float w = 0.f;
+#pragma unroll
+    for (int t = 0; t < L::TILES; ++t) {
+      float sum = 0.f;
+#pragma unroll
+      for (int y = 0; y < RT; ++y) {
+        const pr_f32x4 st = rows_products<E, D, false>(b.k[t], qf[y]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[y][r]));
+          sum += whole || key0 + 16 * t + l16 <= lim[y][r] ? p : 0.f;
+        }
+      }
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      w = g == t ? sum : w;
+    }
+    if (b.to != nullptr) *b.to = b.before + w;
+  };
+  while (key < end) {
+    if (key + STEP < end) load(b1, key + STEP);
+    compute(b0, key);
+    key += STEP;
+    if (key >= end) break;
+    if (key + STEP < end) load(b0, key + STEP);
+    compute(b1, key);
+    key += STEP;
   }
 }
 
@@ -378,6 +492,19 @@ static bool weigh_tiles_as(const PagedArgs& a, const void* q, const float* lse, 
 
 template <typename E, int D>
 static bool weigh_as(const PagedArgs& a, const void* q, const float* lse, int accumulate, hipStream_t s) {
+  const long long rows = (long long)a.max_new * (a.h_q / a.h_kv);
+  if (rows <= WT_FROM_ROWS) {  // what weigh_stream_kernel holds
+    constexpr int STEP = PW_NW * RowsLayout<E, D>::BK;
+    const long long heads = (long long)a.n_seqs * a.h_kv;
+    const long long want = (heads * a.max_len / (4ll * device_cu_count()) + STEP - 1) / STEP * STEP;  // four workgroups per compute unit
+    const int entries = (int)std::max<long long>(STEP, std::min<long long>(want, WS_MOST));
+    const long long all = ((long long)a.max_len + entries - 1) / entries * heads;
+    if (all * PW_NW * 64 > PAGED_MAX_THREADS) return false;
+    const dim3 grid((unsigned)all), block(PW_NW * 64);
+    if (rows <= 16) hipLaunchKernelGGL((weigh_stream_kernel<E, D, 1>), grid, block, 0, s, a, q, lse, accumulate, entries);
+    else hipLaunchKernelGGL((weigh_stream_kernel<E, D, 2>), grid, block, 0, s, a, q, lse, accumulate, entries);
+    return true;
+  }
   constexpr int KEYS = PW_NW * 16 * pw_tiles<E>();
   const long long blocks = ((long long)a.max_len + KEYS - 1) / KEYS, all = blocks * a.n_seqs * a.h_kv;
   if (all * PW_NW * 64 > PAGED_MAX_THREADS) return false;

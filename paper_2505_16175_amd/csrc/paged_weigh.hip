@@ -218,8 +218,6 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
   }
 }
 
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
-
 constexpr int WT_NW = 4;                 // wavefronts of a workgroup
 constexpr int WT_KEYS = WT_NW * 64;      // and its entries
 constexpr int WT_SLOTS = 4;
@@ -247,7 +245,7 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
   __shared__ __attribute__((aligned(16))) float neg[WT_ROWS];  // -lse of the segment's rows, base 2
   __shared__ int dead[WT_ROWS / 32];                           // a row of the tile saw nothing
   constexpr int ROWB = F8 ? 128 : 256;
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int x = blockIdx.x;
   const int h = x % a.h_kv;
@@ -263,27 +261,27 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
   const int rows = q.n * r_heads;
   const int mask = (1 << a.page_shift) - 1;
 
-  // this lane's two entries: their keys, and the first row that sees them
-  pr_u32x4 k[2][8];
-  size_t at[2];
-  bool here[2];
-  int first_row[2];
+  // this lane's four entries: their keys, and the first row that sees them; it stores the one of tile g
+  pr_u32x4 k[4][4];
+  size_t mine_at = 0;
+  bool mine = false;
+  int first_row[4];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int key = key0 + 32 * b + l32, kc = min(key, q.len - 1);
+  for (int b = 0; b < 4; ++b) {
+    const int key = key0 + 16 * b + l16, kc = min(key, q.len - 1);
     const int page = a.table[(size_t)s * a.table_pages + (kc >> a.page_shift)];
     const bool ok = paged_page_ok(page, a.n_pages);
-    here[b] = ok && key < q.len;
-    at[b] = paged_row(ok ? page : 0, h, kc & mask, a.h_kv, a.page_shift);
+    const size_t at = paged_row(ok ? page : 0, h, kc & mask, a.h_kv, a.page_shift);
+    if (g == b) mine_at = at, mine = ok && key < q.len;
     first_row[b] = paged_clamp(key - q.base, 0, q.n) * r_heads;
-    const unsigned char* p = (const unsigned char*)a.k + at[b] * ROWB;
+    const unsigned char* p = (const unsigned char*)a.k + at * ROWB;
 #pragma unroll
-    for (int st = 0; st < 8; ++st) {
+    for (int st = 0; st < 4; ++st) {
       if constexpr (F8) {
-        const uint2 raw = *(const uint2*)(p + 16 * st + 8 * g);
+        const uint2 raw = *(const uint2*)(p + 32 * st + 8 * g);
         k[b][st] = pr_widen8(raw.x, raw.y);
       } else {
-        k[b][st] = *(const pr_u32x4*)(p + 32 * st + 16 * g);
+        k[b][st] = *(const pr_u32x4*)(p + 64 * st + 16 * g);
       }
     }
   }
@@ -293,12 +291,12 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
   const int begin = min(tile_first + split * per, tile_end), end = min(begin + per, tile_end);
   const int masked_below = paged_clamp(key0 + 63 - q.base, 0, q.n) * r_heads;  // rows below do not see all of the wavefront's entries
 
-  int q_addr[8];  // query fragment of step st: row l32, chunk 2 st + g at position (2 st + g) ^ (l32 & 15)
+  int q_addr[4];  // query fragment of step st: row l16, chunk 4 st + g at position (4 st + g) ^ l16; rows 16 .. 31 alike
 #pragma unroll
-  for (int st = 0; st < 8; ++st) q_addr[st] = l32 * 256 + (((2 * st + g) ^ (l32 & 15)) << 4);
+  for (int st = 0; st < 4; ++st) q_addr[st] = l16 * 256 + (((4 * st + g) ^ l16) << 4);
   const unsigned ring = lds_address(smem);
   const float c2 = a.scale_log2;
-  float sum[2] = {0.f, 0.f};
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
 
   for (int seg = begin; seg < end; seg += WT_ROWS / 32) {  // tiles of a segment
     const int seg_end = min(end, seg + WT_ROWS / 32);
@@ -372,66 +370,58 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
       asm volatile("" ::: "memory");
       if (i + 3 < n) request((i + 3) & 3);
       const unsigned char* const slot = smem + (i & 3) * WT_TILE;
-      pr_u32x4 qf[8];
-#pragma unroll
-      for (int st = 0; st < 8; ++st) qf[st] = *(const pr_u32x4*)(slot + q_addr[st]);
-      float4 ng[4];  // of rows 8 y + 4 g ..
-#pragma unroll
-      for (int y = 0; y < 4; ++y) ng[y] = *(const float4*)&neg[i * 32 + 8 * y + 4 * g];
-      f32x16 sc[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[b][r] = 0.f;
-#pragma unroll
-        for (int st = 0; st < 8; ++st)
-          sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pr_bf16x8, qf[st]),
-                                                          __builtin_bit_cast(pr_bf16x8, k[b][st]), sc[b], 0, 0, 0);
-      }
       const int tile_row = row0 + i * 32;
       const bool whole = tile_row >= masked_below && tile_row + 32 <= rows && __builtin_amdgcn_readfirstlane(dead[i]) == 0;
-      if (whole) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float acc = 0.f;
+      for (int y = 0; y < 2; ++y) {
+        pr_u32x4 qf[4];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 0], c2, ng[y].x));
-            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 1], c2, ng[y].y));
-            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 2], c2, ng[y].z));
-            acc += __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + 3], c2, ng[y].w));
+        for (int st = 0; st < 4; ++st) qf[st] = *(const pr_u32x4*)(slot + q_addr[st] + 4096 * y);
+        const float4 ng = *(const float4*)&neg[i * 32 + 16 * y + 4 * g];
+        pr_f32x4 sc[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) sc[b] = pr_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+            sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, qf[st]),
+                                                            __builtin_bit_cast(pr_bf16x8, k[b][st]), sc[b], 0, 0, 0);
+        if (whole) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[b][0], c2, ng.x)), p1 = __builtin_amdgcn_exp2f(fmaf(sc[b][1], c2, ng.y));
+            const float p2 = __builtin_amdgcn_exp2f(fmaf(sc[b][2], c2, ng.z)), p3 = __builtin_amdgcn_exp2f(fmaf(sc[b][3], c2, ng.w));
+            sum[b] += (p0 + p1) + (p2 + p3);
           }
-          sum[b] += acc;
-        }
-      } else {
+        } else {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float acc = 0.f;
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
+          for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float z = e == 0 ? ng[y].x : e == 1 ? ng[y].y : e == 2 ? ng[y].z : ng[y].w;
-              const int r = tile_row + 8 * y + 4 * g + e;
+              const float z = e == 0 ? ng.x : e == 1 ? ng.y : e == 2 ? ng.z : ng.w;
+              const int r = tile_row + 16 * y + 4 * g + e;
               const bool seen = r >= first_row[b] && r < rows && z != -INFINITY;
-              const float p = __builtin_amdgcn_exp2f(fmaf(sc[b][4 * y + e], c2, z));
-              acc += seen ? p : 0.f;
+              const float p = __builtin_amdgcn_exp2f(fmaf(sc[b][e], c2, z));
+              sum[b] += seen ? p : 0.f;
             }
-          sum[b] += acc;
         }
       }
     }
   }
+  float w = 0.f;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const float w = sum_halves(sum[b]);
-    if (g != b || !here[b]) continue;
-    if (o.splits > 1) {
-      o.partial[(((size_t)split * a.n_seqs + s) * a.h_kv + h) * a.max_len + key0 + 32 * b + l32] = w;
-    } else {
-      float* const to = a.weight + at[b];
-      *to = o.accumulate ? *to + w : w;
-    }
+  for (int b = 0; b < 4; ++b) {
+    float x = sum[b] + __shfl_xor(sum[b], 16, 64);
+    x += __shfl_xor(x, 32, 64);
+    w = g == b ? x : w;
+  }
+  if (!mine) return;
+  if (o.splits > 1) {
+    o.partial[(((size_t)split * a.n_seqs + s) * a.h_kv + h) * a.max_len + key0 + lane] = w;
+  } else {
+    float* const to = a.weight + mine_at;
+    *to = o.accumulate ? *to + w : w;
   }
 }
 

@@ -11,10 +11,11 @@
 //
 // weigh_tile_kernel: chunks over bf16 heads of 128. Four wavefronts own 64 entries each, keys in registers, and walk the rows 32 at a
 // time, which all of them read from LDS: tiles of queries go global -> LDS directly (XOR-swizzled 16-byte chunks), in a ring of four
-// slots, three ahead, one barrier each. Bound by the vector unit: a pair costs a multiply-add, an exponential at a quarter of the
-// rate and an add, 24 cycles per 64 pairs, beside the products' 16 on the matrix pipe. 500 tokens of the 7B heads over 46,125 entries
-// (one question): 98 us of exponentials, multiply-adds and adds at 2.4 GHz, 204 measured. Two wavefronts per SIMD that keep a second set of
-// scores, so that one tile's exponentials stand beside the next one's products, took 217-222, a barrier for every second tile the same.
+// slots, three ahead, one barrier each. A pair costs a multiply-add, an exponential at a quarter of the rate and an add, 24 cycles per
+// 64 pairs of the vector unit, beside the products' 16 on the matrix pipe: 98 and 66 us at 2.4 GHz for 500 tokens of the 7B heads over
+// 46,125 entries (one question), which take 193. The clock that the card keeps under both sets that: products of 32 x 32 x 16, the same work at
+// more power, took 205-208, but four wavefronts per SIMD instead of three 194-195, and before that two with a second set of scores, so that
+// one tile's exponentials stood beside the next one's products, 217-222, with a barrier for every second tile the same.
 #include "paged_rows.h"
 
 #include <algorithm>

@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t order_key(float s) {
 }
 
 struct SelectLds {
-  __attribute__((aligned(8))) uint32_t hist[SEL_NB];  // zero at entry, and again when the search returns
+  __attribute__((aligned(16))) uint32_t hist[SEL_NB];  // 16: wave_a then is too, which is read by fours. Zero at entry, and again when the search returns
   uint32_t list[SEL_LIST];
   uint32_t wave_a[SEL_WAVES];
   uint32_t sel_bucket, sel_need, sel_count, sel_key, list_n;  // list_n: zero at entry

@@ -563,12 +563,20 @@ class PagedBatch:
         self.n_seqs, self.n_rows, self.device_index = n_seqs, n_rows, here
         self.c = qp_paged_batch(*at, n_seqs, page_table.shape[1], n_rows, n_rows if max_new is None else max_new, max_len or 0)
         self.ref = ctypes.byref(self.c)
+        self.refs = {}                                   # page_tokens -> a struct of its own, where no max_len is stated
 
     def of(self, cache):
-        """The struct for a pool, whose pages say what a sequence of the batch can hold where it states no max_len."""
-        if self.max_len is None:
-            self.c.max_len = min(self.c.table_pages * cache.c.page_tokens, 1 << 30)
-        return self.ref
+        """The struct for a pool, whose pages say what a sequence of the batch can hold where it states no max_len. A struct once
+        handed out is never written again: calls run without the interpreter's lock, and another thread's may be reading it."""
+        if self.max_len is not None:
+            return self.ref
+        page_tokens = cache.c.page_tokens
+        ref = self.refs.get(page_tokens)
+        if ref is None:
+            c = qp_paged_batch.from_buffer_copy(self.c)
+            c.max_len = min(c.table_pages * page_tokens, 1 << 30)
+            ref = self.refs[page_tokens] = ctypes.byref(c)
+        return ref
 
 
 def _same_gpu(layout, cache, batch):

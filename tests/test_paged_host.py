@@ -2,6 +2,7 @@
 import ctypes
 import os
 import subprocess
+import types
 
 import numpy as np
 import pytest
@@ -112,6 +113,42 @@ def test_plans_cover_the_entries_and_fit_what_is_offered(layout):
     assert B.paged_workspace_bytes(L, 0, 1, 1, 1) == 0 and B.paged_workspace_bytes(L, 1, 1, 1, 0) == 0
     assert B.paged_workspace_bytes(L, 1, 1, 1, 1, -1) == 0
     assert B.paged_workspace_bytes(L, 3, 0, 0, 60000, 1000) >= 4 * 3 * layout[1] * 60000 > B.paged_workspace_bytes(L, 3, 0, 0, 60000, 0)
+
+
+class _Tensor:
+    """What the binding looks at of a tensor on the GPU."""
+
+    def __init__(self, *shape, dtype=torch.int32):
+        self.shape, self.dtype = torch.Size(shape), dtype
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return FAKE
+
+
+def test_a_batch_without_max_len_is_as_long_as_each_pools_pages_whoever_else_uses_it():
+    """Two threads may use one batch over pools of different pages: what one call was handed does not change under it."""
+    batch = B.PagedBatch(_Tensor(2, 5), _Tensor(2), _Tensor(3), n_rows=7)
+    small, large = (types.SimpleNamespace(c=B.qp_paged_cache(page_tokens=p)) for p in (16, 128))
+    read = lambda ref: ctypes.cast(ref, ctypes.POINTER(B.qp_paged_batch)).contents
+    first = batch.of(small)
+    second = batch.of(large)
+    assert read(first).max_len == 80 and read(second).max_len == 640
+    assert read(batch.of(small)).max_len == 80
+    for b in (read(first), read(second)):
+        assert (b.page_table, b.len, b.row_start, b.n_seqs, b.table_pages, b.n_rows, b.max_new) == (FAKE, FAKE, FAKE, 2, 5, 7, 7)
+    stated = B.PagedBatch(_Tensor(2, 5), _Tensor(2), _Tensor(3), n_rows=7, max_new=3, max_len=33)
+    assert read(stated.of(small)).max_len == read(stated.of(large)).max_len == 33 and read(stated.of(small)).max_new == 3
+    huge = B.PagedBatch(_Tensor(1, 1 << 28), _Tensor(1))
+    assert read(huge.of(large)).max_len == 1 << 30
 
 
 # ---- the oracle, by hand ----

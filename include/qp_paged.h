@@ -81,7 +81,9 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
 /* Attention of the new tokens: q, out [n_rows][H_q][d] (layout dtype), lse_or_null [H_q][n_rows] f32 (natural log). A row that
  * sees no entry (the sequence has fewer than its new rows, or none of its pages is there) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (few rows: to two bf16 terms),
- * never in the sums behind lse. What a row does not see does not reach its result, infinities and NaN included.
+ * never in the sums behind lse. What a row does not see does not reach its result, infinities and NaN included. Logits scale * q.k of
+ * up to 2^28 in size are computed; those below -2^29 weigh nothing, as -infinity does, and a row that sees nothing else is one that sees
+ * no entry; of a row with one above 2^28 nothing is promised.
  *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups
  *     whose partial results (f32) lie there until a second launch merges them; without it (or with less) to fewer. */
 qp_status qp_paged_attend(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, const void* q,

@@ -592,7 +592,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   float l_run = 0.f;        // this lane's share of the row's denominator
   const float c2 = a.scale_log2;
   float nmc = 0.f;  // -m_run * c2
-  const float lowest = -1e30f / fmaxf(c2, 1.f);  // PAGED: finite, and so is its product with c2
+  const float lowest = fmaxf(PR_NONE / c2, -FLT_MAX);  // PAGED: the lowest reference of the arithmetic for few rows, and why
 
   // Moves the reference to the rows' max including this block, rescales what was summed so far and forms the block's
   // numerators (first block of a row, and blocks whose numerators outgrew the reference). look: the max of the tile's other

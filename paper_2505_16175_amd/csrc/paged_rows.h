@@ -113,7 +113,10 @@ __device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout
   return s;
 }
 
-constexpr float PR_NONE = -3e38f;  // a row's reference (log2 units) before its first visible entry
+// A row's reference (log2 units) before its first visible entry, and its lowest one. c s - m is one multiply-add, so with m rounded from
+// a product all numerators of a row carry the same factor, 2 to the power of what that rounding lost: it cancels as long as it is finite. A
+// block of nothing but huge negative logits would make it 2^(2^-24 |m|), an infinity that no later reference takes back.
+constexpr float PR_NONE = -0x1p29f;
 constexpr float PR_LAZY = 8.f;
 
 template <typename E, int D>

@@ -645,3 +645,98 @@ def test_a_pool_beyond_32_bits():
     for h in range(8):
         assert torch.equal(cache.k[n_pages - 2, h], k[kept[0, h, :256].long(), h])
         assert torch.equal(cache.v[n_pages - 5, h, :44], v[kept[0, h, 256:].long(), h])
+
+
+# ---- against a plain implementation in 64 bits on the GPU ----
+
+def plain(sc, lse=None, absent=()):
+    """What P.attend returns and, for given lse, the weights that the rows add to every entry of the pool: sequence by sequence and head
+    by head in 64 bits. absent: pages whose entries count as not there."""
+    n, h_q, d, r = sc.n_rows, sc.h_q, sc.d, sc.h_q // sc.h_kv
+    f64 = dict(dtype=torch.float64, device=DEV)
+    out, absv, size = torch.full((n, h_q, d), math.nan, **f64), torch.zeros(n, h_q, d, **f64), torch.zeros(h_q, n, **f64)
+    wl = torch.full((h_q, n), math.nan, **f64)
+    added = torch.zeros(sc.cache.weight.shape, **f64)
+    q = sc.q.to(DEV).double()
+    for s, (length, begin, new) in enumerate(zip(sc.lens, sc.starts, sc.new)):
+        j, page, slot = P.places(sc.table[s].numpy(), length, sc.page, sc.cache.c.n_pages)
+        here = ~np.isin(page, absent)
+        j, page, slot = (torch.tensor(x[here], device=DEV) for x in (j, page, slot))
+        limit = (length - new + torch.arange(new, device=DEV)).repeat_interleave(r)
+        for h in range(sc.h_kv):
+            heads = slice(h * r, h * r + r)
+            k, v = (t[page, h, slot].float().double() for t in (sc.cache.k, sc.cache.v))
+            rows = q[begin:begin + new, heads].reshape(new * r, d)
+            x = sc.scale * (rows @ k.t())
+            seen = j[None] <= limit[:, None]
+            top = (sc.scale * (rows.abs() @ k.abs().t()) + x.abs()).masked_fill(~seen, 0)
+            x = x.masked_fill(~seen, -math.inf)
+            some = seen.any(1, keepdim=True)
+            p = torch.where(some, torch.softmax(x.masked_fill(~some, 0), 1), 0)
+            put = lambda y: y.view(new, r, -1)
+            out[begin:begin + new, heads], absv[begin:begin + new, heads] = put(p @ v), put(p @ v.abs())
+            wl[heads, begin:begin + new] = torch.logsumexp(x, 1).view(new, r).t()
+            size[heads, begin:begin + new] = (top.amax(1) if len(j) else top.sum(1)).view(new, r).t()
+            if lse is not None:
+                z = lse[heads, begin:begin + new].t().reshape(-1, 1).double()
+                added[page, h, slot] = torch.where(z > -math.inf, torch.exp(x - torch.where(z > -math.inf, z, 0)), 0).sum(0)
+    return out, wl, absv, size, added
+
+
+def check_plain(sc, out, lse, want, what=""):
+    """The tolerances of check_attend."""
+    wo, wl, absv, size, _ = want
+    e = (sc.d + 16) * U * size + 2.0 ** -22
+    rows = ~torch.isnan(wl).all(0)
+    assert (out[~rows] == 7.0).all() and (lse[:, ~rows] == 7.0).all(), f"{what}: rows of nobody were written"
+    tol = sc.h * wo.abs() + absv * (2 * e.t()[:, :, None] + (NUMERATORS(sc) or (0.0 if sc.h == U else 2.0 ** -16)) + 2.0 ** -15) + 1e-30
+    off = ((out.double() - wo).abs() / tol)[rows]
+    assert (off <= 1).all(), f"{what}: off by {off.max():.2f} tolerances"
+    none = torch.isneginf(wl[:, rows])
+    assert torch.equal(torch.isneginf(lse[:, rows]), none) and (out[rows].double()[none.t()] == 0).all()
+    off = ((lse.double() - wl).abs() / (2 * e + 2.0 ** -16 + 4 * U * wl.abs()))[:, rows][~none]
+    assert (off <= 1).all(), f"{what}: lse off by {off.max():.2f} tolerances"
+
+
+# ---- logits of any size ----
+
+@pytest.mark.parametrize("layout", [TINY, F32, BF64, L7, L72])
+@pytest.mark.parametrize("new", [2, 50])
+def test_whole_blocks_of_lowest_logits(layout, new):
+    """Pages of keys whose products with every query are far below zero, of sizes from 1e10 to 1e33: e to that is 0, so rows weigh the other entries
+    as if those were not there, whether the low ones come first or later, and rows that see nothing else see nothing."""
+    sc = Scene(layout, 64, [400, 130, 70], [new, new, new], seed=new)
+    sc.q.abs_()
+    low = [int(sc.table[s, b]) for s, b in ((0, 0), (0, 1), (0, 4), (1, 1), (2, 0), (2, 1))]
+    g = torch.Generator().manual_seed(3)
+    for page in low:
+        size = 10.0 ** (10 + 23 * torch.rand(sc.h_kv, 64, 1, generator=g))
+        sc.cache.k[page] = (-size).to(sc.q.dtype).to(DEV)
+        sc.cache.v[page] = 1.0
+    want = plain(sc, absent=low)
+    for ws in ("full", None):
+        out, lse = sc.attend(ws)
+        check_plain(sc, out, lse, want, f"{ws}")
+    B.paged_weigh(sc.layout, sc.cache, sc.batch, sc.q.to(DEV), lse, False, sc.ws)
+    torch.cuda.synchronize()
+    assert (sc.cache.weight[low[:4]] == 0).all()
+
+
+@pytest.mark.parametrize("layout", [TINY, BF64, L7])
+@pytest.mark.parametrize("new", [2, 50])
+def test_one_logit_above_all_others(layout, new):
+    """An entry whose logits of up to 2^28 leave the others nothing: the rows are its value, and lse its logit."""
+    sc = Scene(layout, 32, [300, 90], [new, new], seed=new)
+    sc.q.abs_().clamp_(max=2.0)
+    at = [(int(sc.table[s, b]), e) for s, b, e in ((0, 3, 7), (1, 0, 31))]
+    for page, e in at:
+        sc.cache.k[page, :, e] = 2.0 ** 28 / (2 * sc.d * sc.scale)
+    out, lse = sc.attend()
+    _, wl, _, _, _ = plain(sc)
+    for s, (page, e) in enumerate(at):
+        rows = slice(sc.starts[s], sc.starts[s + 1])
+        v = sc.cache.v[page, :, e].double().repeat_interleave(sc.h_q // sc.h_kv, 0)[None]
+        assert (wl[:, rows] > 2.0 ** 24).all()
+        assert ((out[rows].double() - v).abs() <= v.abs() * (sc.h + (NUMERATORS(sc) or 2.0 ** -16) + 2.0 ** -15)).all()
+        # the product's sum, the scale times log2 e, its product and the one back to base e
+        assert ((lse[:, rows].double() - wl[:, rows]).abs() <= (sc.d + 8) * U * wl[:, rows]).all()

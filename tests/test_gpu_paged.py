@@ -698,6 +698,119 @@ def check_plain(sc, out, lse, want, what=""):
     assert (off <= 1).all(), f"{what}: lse off by {off.max():.2f} tolerances"
 
 
+def check_plain_weights(sc, lse, ws, what=""):
+    """The tolerances of check_weigh, taken anew and then added to that."""
+    want = plain(sc, lse)
+    size = want[3].max() + lse[torch.isfinite(lse)].abs().max()
+    e = float((sc.d + 16) * U * size) + 2.0 ** -22 + (max(sc.new) * (sc.h_q // sc.h_kv) + 4) * U
+    live = torch.zeros(sc.cache.weight.shape, dtype=torch.bool, device=DEV)
+    for s, n in enumerate(sc.lens):
+        _, page, slot = P.places(sc.table[s].numpy(), n, sc.page, sc.cache.c.n_pages)
+        live[torch.tensor(page, device=DEV), :, torch.tensor(slot, device=DEV)] = True
+    for accumulate in (False, True):
+        before = sc.cache.weight.clone()
+        B.paged_weigh(sc.layout, sc.cache, sc.batch, sc.q.to(DEV), lse, accumulate, ws)
+        torch.cuda.synchronize()
+        full = want[4] + (before.double() if accumulate else 0)
+        err = (sc.cache.weight.double() - full).abs()[live]
+        tol = (want[4] * e + 2 * U * full.abs() + 1e-37)[live]
+        assert (err <= tol).all(), f"{what}: weights off by {(err / tol).max():.2f} tolerances"
+        assert torch.equal(sc.cache.weight[~live], before[~live]), f"{what}: weights of nobody were written"
+
+
+# ---- long chunks ----
+
+@pytest.mark.parametrize("layout,page,lens,new,more", [
+    (L7, 64, [1500, 700], [1300, 650], {}),                                    # 9,100 and 4,550 stacked rows
+    (L7, 16, [900, 1250], [1210, 37], dict(missing=[(0, 5), (1, 70)])),        # 8,470 rows, of which the first 2,170 see nothing
+    (L72, 128, [1025, 600], [1025, 513], dict(fp8=True)),                      # 8,200 and 4,104
+    (ODD, 32, [2900], [2801], {})])                                            # 8,403
+def test_chunks_of_more_rows_than_one_lot_of_statistics(layout, page, lens, new, more):
+    """Weighing keeps the statistics of 4,096 stacked rows in LDS: here a workgroup goes through several such lots, in the later
+    ones too with rows that saw nothing, and starts in any of them where it has the workspace. Attention of the same rows has row
+    blocks that end in front of a key chunk."""
+    sc = Scene(layout, page, lens, new, seed=len(lens) + page, **more)
+    want = plain(sc)
+    assert B.paged_plan(sc.layout, sc.cache, sc.batch, sc.ws.numel())["key_chunks"] > 1
+    for ws in ("full", None):
+        print("attend", ws, flush=True)
+        out, lse = sc.attend(ws)
+        check_plain(sc, out, lse, want, f"{ws}")
+    r = sc.h_q // sc.h_kv
+    for row in (sc.starts[1] - 1, sc.starts[0] + 4100 // r, sc.starts[0] + 8190 // r if new[0] * r > 8190 else sc.starts[0]):
+        lse[1::3, row] = -math.inf
+    for ws in (sc.ws, None):
+        print("weigh", ws is None, flush=True)
+        check_plain_weights(sc, lse, ws, "without workspace" if ws is None else "")
+
+
+@pytest.mark.parametrize("layout,page,lens,new,fp8", [(L7, 16, [5003, 1100], [40, 9], False), (L72, 16, [3999, 2300], [33, 5], True), (L7, 32, [9000], [77], False)])
+def test_chunks_over_more_pages_than_one_list(layout, page, lens, new, fp8):
+    """The tile kernel has 64 page numbers of a table at hand: here it goes on to the next ones inside its loop, over pages that
+    are missing where one list ends and the next begins, and over more missing ones in a row than a list has."""
+    per = lens[0] // page
+    missing = [(0, b) for b in (0, 1, 63, 64, per // 2 - 1)] + [(0, b) for b in range(126, min(201, per - 3))] + [(s, 62) for s in range(1, len(lens))]
+    sc = Scene(layout, page, lens, new, seed=page + len(lens), fp8=fp8, missing=missing)
+    want = plain(sc)
+    two_chunks = 2 * sc.n_rows * sc.h_q * 129 * 4
+    outs = []
+    for ws in ("full", None, sc.ws[: -(-two_chunks // 256) * 256]):
+        plan = B.paged_plan(sc.layout, sc.cache, sc.batch, sc.ws.numel() if isinstance(ws, str) else 0 if ws is None else ws.numel())
+        print("attend", plan, flush=True)
+        assert plan["rows_per_tile"] == 256 and (plan["key_chunks"] > 2 if isinstance(ws, str) else plan["key_chunks"] == (1 if ws is None else 2))
+        out, lse = sc.attend(ws)
+        check_plain(sc, out, lse, want, str(plan))
+        outs.append((out, lse))
+    for ws, (out, lse) in zip(("full", None), outs):
+        again, z = sc.attend(ws)
+        assert torch.equal(again, out) and torch.equal(z, lse)                  # the same bits
+    for ws in (sc.ws, None):
+        check_plain_weights(sc, lse, ws, "without workspace" if ws is None else "")
+
+
+# ---- limits ----
+
+@pytest.mark.parametrize("starts", [[2, 5, 7], [-7, 3, 2 ** 31 - 1], [5, 2, 7], [2 ** 31 - 1, -2 ** 31, 4], [1, 6, 10]])
+@pytest.mark.parametrize("layout", [L7, TINY, L72])
+def test_rows_beyond_the_limits_are_left_alone(layout, starts):
+    """Whose rows are whose when the device says something odd, from the documented limits: first row into [0, n_rows], end from
+    there to n_rows, max_new rows of them. Those are written, no other ones, and append changes those entries alone."""
+    sc = Scene(layout, 16, [60, 100], [3, 2], seed=5)
+    n, big, max_new, max_len = sc.n_rows, [2 ** 31 - 1, 41], 3, 48
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    batch = B.PagedBatch(sc.table.to(DEV), i32(big), i32(starts), n, max_new=max_new, max_len=max_len)
+    owned, entries = {}, {}
+    for s in range(2):
+        length = min(max(big[s], 0), max_len, sc.table.shape[1] * 16)
+        r0 = min(max(starts[s], 0), n)
+        count = min(max(starts[s + 1], r0), n) - r0
+        for i in range(min(count, max_new)):
+            j = length - count + i
+            page = int(sc.table[s, j // 16]) if j >= 0 else -1
+            owned[r0 + i] = page >= 0
+            if page >= 0:
+                entries[page, j % 16] = r0 + i
+    out, lse = sc.q.to(DEV), torch.full((sc.h_q, n), 7.0, device=DEV)
+    out = torch.full_like(out, 7.0)
+    B.paged_attend(sc.layout, sc.cache, batch, sc.q.to(DEV), out, lse, sc.ws)
+    torch.cuda.synchronize()
+    for row in range(n):
+        if row not in owned:
+            assert (out[row] == 7.0).all() and (lse[:, row] == 7.0).all(), row
+        elif owned[row]:
+            assert (out[row] != 7.0).any(-1).all() and torch.isfinite(lse[:, row]).all() and (lse[:, row] != 7.0).all(), row
+        else:
+            assert (out[row] == 0).all() and torch.isneginf(lse[:, row]).all(), row
+    k = torch.full((n, sc.h_kv, sc.d), 5.0, dtype=sc.q.dtype, device=DEV)
+    before = [x.clone() for x in (sc.cache.k, sc.cache.v, sc.cache.pos, sc.cache.weight)]
+    B.paged_append(sc.layout, sc.cache, batch, k, -k, torch.arange(-1000, -1000 + n, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    for (page, slot), row in entries.items():
+        before[0][page, :, slot], before[1][page, :, slot], before[2][page, :, slot], before[3][page, :, slot] = 5, -5, row - 1000, 0
+    for x, y in zip((sc.cache.k, sc.cache.v, sc.cache.pos, sc.cache.weight), before):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
 # ---- logits of any size ----
 
 @pytest.mark.parametrize("layout", [TINY, F32, BF64, L7, L72])

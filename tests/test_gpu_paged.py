@@ -853,3 +853,69 @@ def test_one_logit_above_all_others(layout, new):
         assert ((out[rows].double() - v).abs() <= v.abs() * (sc.h + (NUMERATORS(sc) or 2.0 ** -16) + 2.0 ** -15)).all()
         # the product's sum, the scale times log2 e, its product and the one back to base e
         assert ((lse[:, rows].double() - wl[:, rows]).abs() <= (sc.d + 8) * U * wl[:, rows]).all()
+
+
+# ---- shared pages, streams ----
+
+def test_sequences_that_share_pages_are_evicted_in_one_call():
+    """Three sequences over one video's pages with tails and lengths of their own: each list is its own, the shared pages stay."""
+    sc = Scene(L7, 16, [100, 100, 100], [0, 0, 0], seed=12, spare_pages=3 * 3 + 1)
+    table = sc.table.clone()
+    table[1:, :4] = table[0, :4]                                                # 64 shared entries
+    lens, keep = [100, 83, 40], 45
+    used = set(x for row in sc.table.tolist() for x in row)
+    free = [p for p in range(sc.cache.c.n_pages) if p not in used]
+    to = torch.tensor([[free.pop() for _ in range(3)] for _ in lens], dtype=torch.int32)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    batch = B.PagedBatch(table.to(DEV), i32(lens))
+    to_len, kept = i32([-1] * 3), torch.full((3, sc.h_kv, keep), 99, dtype=torch.int32, device=DEV)
+    before = sc.pool()
+    B.paged_evict(sc.layout, sc.cache, batch, keep, 2, 5, to.to(DEV), to_len, kept, B.make_paged_workspace(sc.layout, batch, keep, 16))
+    torch.cuda.synchronize()
+    got, want = sc.pool(), P.evict(before, table.tolist(), lens, keep, 2, 5)
+    assert to_len.tolist() == [45, 45, 40]
+    for s in range(3):
+        for h in range(sc.h_kv):
+            w = want[s * sc.h_kv + h]
+            np.testing.assert_array_equal(kept[s, h, :len(w)].cpu().numpy(), w)
+            x = np.arange(len(w))
+            for name in got:
+                np.testing.assert_array_equal(got[name][to[s].numpy()[x // 16], h, x % 16], before[name][table[s].numpy()[w // 16], h, w % 16])
+    kept_pages = [p for p in range(sc.cache.c.n_pages) if p not in to.flatten().tolist()]
+    for name in got:
+        np.testing.assert_array_equal(got[name][kept_pages], before[name][kept_pages])
+
+
+def test_calls_on_two_streams_at_once():
+    """Two batches over one pool, each on a stream and with a workspace of its own: the bits that either gives alone."""
+    sc = Scene(L7, 32, [9000, 700, 5000, 300], [1, 2, 60, 40], seed=13)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    q = sc.q.to(DEV)
+    halves = []
+    for a, b in ((0, 2), (2, 4)):
+        batch = B.PagedBatch(sc.table[a:b].to(DEV), i32(sc.lens[a:b]), i32(sc.starts[a:b + 1]), sc.n_rows, max_new=max(sc.new[a:b]))
+        halves.append((batch, B.make_paged_workspace(sc.layout, batch, 200, 32), torch.cuda.Stream()))
+    weight = sc.cache.weight.clone()
+
+    def calls(half, results):
+        batch, ws, _ = half
+        out, lse = torch.full_like(q, 7.0), torch.full((sc.h_q, sc.n_rows), 7.0, device=DEV)
+        results += [out, lse]
+        for _ in range(3):
+            B.paged_attend(sc.layout, sc.cache, batch, q, out, lse, ws)
+            B.paged_weigh(sc.layout, sc.cache, batch, q, lse, True, ws)
+
+    alone = []
+    for half in halves:
+        calls(half, alone)
+        torch.cuda.synchronize()
+    alone.append(sc.cache.weight.clone())
+    sc.cache.weight.copy_(weight)
+    torch.cuda.synchronize()
+    both = []
+    for half in halves:
+        with torch.cuda.stream(half[2]):
+            calls(half, both)
+    torch.cuda.synchronize()
+    for x, y in zip(alone, both + [sc.cache.weight]):
+        assert torch.equal(x, y)

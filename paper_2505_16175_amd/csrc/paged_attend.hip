@@ -37,7 +37,7 @@ struct PagedOut {
 
 // Two workgroups per compute unit where a block's registers leave room for it. Of bf16 heads of 128 one has the registers to itself:
 // squeezed into half of them its results and addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26.
-template <typename E, int D, int RT>
+template <typename E, int D>
 constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 
 // Where the workgroups' results meet.
@@ -157,7 +157,7 @@ __device__ __forceinline__ int unit_blocks(const PagedArgs& a, const PagedSeq& q
 }
 
 template <typename E, int D, int RT>
-__global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D, RT>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
+__global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
   constexpr int ROWS = 16 * RT, STEP = PR_NW * RowsLayout<E, D>::BK;
   __shared__ RowsLds<D, ROWS> lds;
   const int tid = threadIdx.x;

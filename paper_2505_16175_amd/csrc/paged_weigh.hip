@@ -28,7 +28,7 @@ constexpr int pw_tiles() { return sizeof(E) == 4 ? 2 : 4; }
 
 template <typename E, int D>
 __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, const void* __restrict__ qp_, const float* __restrict__ lse,
-                                                                int accumulate, int blocks) {
+                                                                int accumulate) {
   using L = RowsLayout<E, D>;
   constexpr int KT = pw_tiles<E>();
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
@@ -497,9 +497,9 @@ static bool weigh_as(const PagedArgs& a, const void* q, const float* lse, int ac
     return true;
   }
   constexpr int KEYS = PW_NW * 16 * pw_tiles<E>();
-  const long long blocks = ((long long)a.max_len + KEYS - 1) / KEYS, all = blocks * a.n_seqs * a.h_kv;
+  const long long all = ((long long)a.max_len + KEYS - 1) / KEYS * a.n_seqs * a.h_kv;
   if (all * PW_NW * 64 > PAGED_MAX_THREADS) return false;
-  hipLaunchKernelGGL((paged_weigh_kernel<E, D>), dim3((unsigned)all), dim3(PW_NW * 64), 0, s, a, q, lse, accumulate, (int)blocks);
+  hipLaunchKernelGGL((paged_weigh_kernel<E, D>), dim3((unsigned)all), dim3(PW_NW * 64), 0, s, a, q, lse, accumulate);
   return true;
 }
 

@@ -56,9 +56,9 @@ typedef struct {
   const int32_t* row_start;  /* device, [n_seqs + 1], not descending; NULL for qp_paged_evict                  */
   int32_t n_seqs;
   int32_t table_pages;       /* row length of page_table                                                       */
-  int32_t n_rows;            /* rows that the call's tensors have                                              */
-  int32_t max_new;           /* no sequence has more new tokens: launches are sized by these two, and what a   */
-  int32_t max_len;           /* sequence has beyond them (or beyond its table) is not looked at                */
+  int32_t n_rows;            /* rows that the call's tensors have, at least 1 (qp_paged_evict has none)        */
+  int32_t max_new;           /* >= 1; no sequence has more new tokens: launches are sized by these two, and    */
+  int32_t max_len;           /* what a sequence has beyond them (or beyond its table) is not looked at         */
 } qp_paged_batch;
 
 /* Workspace that every call below accepts for batches of these sizes (256-byte aligned where it is handed over): partial
@@ -80,8 +80,9 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
 
 /* Attention of the new tokens: q, out [n_rows][H_q][d] (layout dtype), lse_or_null [H_q][n_rows] f32 (natural log). A row that
  * sees no entry (the sequence has fewer than its new rows, or none of its pages is there) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
- * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (few rows: to two bf16 terms),
- * never in the sums behind lse. What a row does not see does not reach its result, infinities and NaN included. Logits scale * q.k of
+ * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (to two bf16 terms in calls of up to
+ * 32 stacked rows, max_new * H_q / H_kv, and over heads of 64), never in the sums behind lse. All rows of a call take the same way, so
+ * a row's last bits depend on max_new. What a row does not see does not reach its result, infinities and NaN included. Logits scale * q.k of
  * up to 2^28 in size are computed; those below -2^29 weigh nothing, as -infinity does, and a row that sees nothing else is one that sees
  * no entry; of a row with one above 2^28 nothing is promised.
  *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups

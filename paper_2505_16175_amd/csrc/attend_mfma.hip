@@ -285,7 +285,10 @@ __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const Paged
 // Args = PagedTileArgs: a chunk of new tokens of each sequence of a batch over its pages (qp_paged.h). One segment: the new
 // tokens are the last entries, so row t sees the entries up to base + t. A wavefront's eight keys of a tile lie in one page, whose
 // number it reads from a register that holds the next 64 of the table; eight keys of a missing page are read from zeros and masked.
-// Denominators are summed in f32 from the unrounded numerators, since lse is an f32 result here.
+// Denominators are summed in f32 from the unrounded numerators, since lse is an f32 result here. The numerators of the product with V
+// are one bf16 term, as in the flat path: a second one, which the arithmetic for few rows has for nothing behind its loads, would be half
+// as many products again in a loop that the products bound. Results over up to 46,125 entries are 1.7e-3 from 64 bits, with two terms 1.6e-3,
+// which is their own rounding.
 template <bool F8, class Args>
 __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   constexpr bool PAGED = std::is_same_v<Args, PagedTileArgs>;

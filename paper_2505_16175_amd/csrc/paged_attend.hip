@@ -35,8 +35,10 @@ struct PagedOut {
   int2* info;      // [units]: first share of a unit and the shares that have blocks of it
 };
 
-// Two workgroups per compute unit where a block's registers leave room for it. Of bf16 heads of 128 one has the registers to itself:
-// squeezed into half of them its results and addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26.
+// Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles spill 13 registers in front of and behind
+// the loop over the keys, not in it. Of bf16 heads of 128 one has the registers to itself: squeezed into half of them its results and
+// addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26. Of f32 heads of 128 too, and two row tiles spill 28
+// registers all the same, four of them stored in the loop.
 template <typename E, int D>
 constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 
@@ -363,7 +365,11 @@ static long long merge_blocks(const PagedArgs& a, const PagedPlan& p) {
   return (((long long)a.max_new * a.h_q + rows - 1) / rows) * a.n_seqs;
 }
 
-// Stacked rows above which bf16 heads of 128 take the tile kernel (attend_mfma.hip), and what its 32-bit arithmetic takes.
+// Stacked rows above which bf16 heads of 128 take the tile kernel (attend_mfma.hip), and what its 32-bit arithmetic takes. A workgroup
+// for few rows holds 32; more of them take the entries once for each 32. us few rows / tiles, 7B heads, one sequence over 46,125
+// entries: 1 token 26.0 / 29.3, 4 (28 rows) 30.9 / 30.9, 5 45.7 / 31.9, 12 61.9 / 35.8; 72B heads 46.0 / 56.6, 49.7 / 58.3, 77.8 / 59.5,
+// 106.9 / 65.4. Of 16 sequences over up to 9,840 the tiles win later, 7B heads 57.8 / 78.7, 64.8 / 79.9, 8 tokens 75.6 / 82.1, 12
+// 94.1 / 86.4; 72B heads 95.2 / 111.0, 110.4 / 112.4, 135.2 / 116.6; over 8-bit pools of the 7B heads not up to 12 (68.3 / 90.0).
 constexpr long long PT_FROM_ROWS = 32, PT_MOST_ROWS = 1 << 26;
 
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes) {
@@ -385,6 +391,9 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
     const long long blocks = units * (((long long)a.max_len + step - 1) / step);
     p.workgroups = units * a.h_kv;
     long long shares = std::min(std::max<long long>(1, (a.fp8 ? 2 : 1) * cus / a.h_kv), blocks);
+    // Of a few blocks a workgroup per unit makes no second launch. us with shares / without, one token: f32 heads of 64 over 128
+    // entries 8.7 / 7.6, 256 11.4 / 8.7, 333 11.2 / 10.8, 600 12.0 / 14.6, 1,200 11.2 / 23.9; 7B heads over 256 8.4 / 8.4 (one launch
+    // both), 333 14.0 / 12.7, 600 14.4 / 15.9, 1,200 15.4 / 22.4, over 8-bit pools 333 13.8 / 11.5, 600 13.9 / 14.2, 1,200 15.8 / 20.2.
     if (units > PR_UNITS || blocks > 0x7fffffff || a.max_len <= 2 * step) return p;
     const size_t per_share = (size_t)a.h_kv * p.tile_rows * (d + 1) * sizeof(float), info = (size_t)units * sizeof(int2);
     shares = std::min(shares, scratch_bytes < info ? 0ll : (long long)((scratch_bytes - info) / per_share) - units);

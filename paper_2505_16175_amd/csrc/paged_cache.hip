@@ -107,7 +107,10 @@ bool launch_paged_append(const PagedArgs& a, const PagedAppend& src, int dtype, 
 // between the two. A thread takes four neighbours of a block of 4096: one page number and one load for the four.
 constexpr uint32_t EV_STAYS = 0xffffffffu;
 constexpr int EV_BLOCK = 4 * SEL_THREADS;
-constexpr int EV_HELD = 12;  // blocks whose keys the workgroup holds in registers; those of longer sequences lie in the workspace
+// Blocks whose keys the workgroup holds for itself; those of longer sequences lie in the workspace. us of a call held / by way of the
+// workspace, 4 heads, a third kept: 3,000 entries 18.0 / 16.1, 9,840 22.1 / 21.9, 20,000 29.0 / 30.1, 46,125 48.0 / 57.6, 49,000 49.7 /
+// 58.8; 16 sequences of 8 heads of up to 8,300 138.9 / 135.7. 60,000 entries, in the workspace, 67.5.
+constexpr int EV_HELD = 12;
 
 size_t paged_evict_keys_bytes(int n_seqs, int h_kv, int max_len) {
   const size_t blocks = ((size_t)max_len + EV_BLOCK - 1) / EV_BLOCK;
@@ -116,7 +119,8 @@ size_t paged_evict_keys_bytes(int n_seqs, int h_kv, int max_len) {
 
 // One workgroup has a head to itself, so an instruction per entry costs time: 46,125 of them 0.3 us. us for 16,384 kept of
 // 46,125 entries of 4 heads, one entry per thread and step, keys in the workspace 75, in LDS and registers 59; weights made into
-// dense keys by a launch of their own 6 and 25.
+// dense keys by a launch of their own 6 and 25. The search has HELD's keys in registers; the loop that writes the list is left rolled by
+// the compiler and reads them back from scratch memory (208 bytes per thread), a block at a time.
 template <bool HELD>
 __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(PagedArgs a, PagedEvict e) {
   __shared__ SelectLds lds;

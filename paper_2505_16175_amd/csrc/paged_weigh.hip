@@ -3,8 +3,9 @@
 //
 // weigh_stream_kernel: few rows (decoding, drafted tokens). Queries and their statistics stay in registers, and a wavefront walks
 // blocks of 32 keys (16 of f32), the next one requested while it works on this: S = Q K^T leaves a lane with one entry (column) and
-// four rows. Bound by the keys' way from HBM: 3.7 TB/s (sums of a large array 4.0), where wavefronts that take 64 keys at once and
-// end reached 3.4 (54 us), and no more with fewer or more workgroups per compute unit.
+// four rows. Bound by the keys' way from HBM: 3.7 TB/s, where wavefronts that take 64 keys at once and end reached 3.4 (54 us), and no
+// more with fewer or more workgroups per compute unit. Attention of the same rows, whose workgroups have equal parts of all
+// entries, reads at 5.0: these have up to `entries` of one sequence each and those behind its end have none.
 //
 // paged_weigh_kernel: chunks over layouts without a tile kernel. A wavefront owns 64 entries (32 of f32) of a KV head, whose keys stay
 // in registers, and walks the sequence's rows 16 at a time.
@@ -13,9 +14,10 @@
 // time, which all of them read from LDS: tiles of queries go global -> LDS directly (XOR-swizzled 16-byte chunks), in a ring of four
 // slots, three ahead, one barrier each. A pair costs a multiply-add, an exponential at a quarter of the rate and an add, 24 cycles per
 // 64 pairs of the vector unit, beside the products' 16 on the matrix pipe: 98 and 66 us at 2.4 GHz for 500 tokens of the 7B heads over
-// 46,125 entries (one question), which take 193. The clock that the card keeps under both sets that: products of 32 x 32 x 16, the same work at
-// more power, took 205-208, but four wavefronts per SIMD instead of three 194-195, and before that two with a second set of scores, so that
-// one tile's exponentials stood beside the next one's products, 217-222, with a barrier for every second tile the same.
+// 46,125 entries (one question), which take 190. The clock stays at 2.4 GHz under it and the matrix pipe is busy for 34 % of the cycles
+// (counters), so the two stand one behind the other and do not overlap. Products of 32 x 32 x 16 took 205-208, four wavefronts per
+// SIMD instead of three 194-195, and before that two with a second set of scores, so that one tile's exponentials should have stood beside the
+// next one's products, 217-222, with a barrier for every second tile the same.
 #include "paged_rows.h"
 
 #include <algorithm>
@@ -440,7 +442,9 @@ __global__ __launch_bounds__(WA_THREADS) void weigh_add_kernel(PagedArgs a, Weig
   *to = o.accumulate ? *to + w : w;
 }
 
-// Rows above which a call takes the tiles (stacked rows of a KV head), and what their 32-bit arithmetic takes.
+// Rows above which a call takes the tiles (stacked rows of a KV head), and what their 32-bit arithmetic takes. weigh_stream_kernel holds
+// 32. us streamed / in tiles: 7B heads, one sequence over 46,125 entries, 1 token 12.1 / 12.6, 4 (28 rows) 15.0 / 12.5, 16 sequences over up
+// to 9,840 28.8 / 31.5 and 34.5 / 31.5; 72B heads over 8-bit pools 12.6 / 20.5, 17.1 / 19.6, 28.8 / 50.1 and 36.9 / 49.7.
 constexpr long long WT_FROM_ROWS = 32, WT_MOST_ROWS = 1 << 26;
 constexpr int WT_MOST_HEADS = 1024;
 static bool weigh_tiled(const PagedArgs& a, int dtype, int d) {

@@ -663,7 +663,7 @@ def plain(sc, lse=None, absent=()):
         here = ~np.isin(page, absent)
         j, page, slot = (torch.tensor(x[here], device=DEV) for x in (j, page, slot))
         limit = (length - new + torch.arange(new, device=DEV)).repeat_interleave(r)
-        for h in range(sc.h_kv):
+        for h in range(sc.h_kv if new else 0):
             heads = slice(h * r, h * r + r)
             k, v = (t[page, h, slot].float().double() for t in (sc.cache.k, sc.cache.v))
             rows = q[begin:begin + new, heads].reshape(new * r, d)

@@ -14,7 +14,7 @@ namespace qp {
 // token (154.5 before) and 260.7 for 64 (268.2).
 // AHEAD doubles the registers of the 16-chunk variant: 3 wavefronts share a SIMD, 5 without (rows of up to 4096: 5 either
 // way). It is the faster one while its wavefronts are all resident at once, 12 tokens per CU. us without / with, 8192
-// elements: 1 token 9.2 / 7.6, 1024 15.2 / 11.7, 3072 23.8 / 22.9, 4096 26.9 / 31.5; 5120 elements: 20.5 / 23.5 at 4096.
+// elements: 1 token 9.2 / 7.6, 1024 15.2 / 11.7, at that limit 23.8 / 22.9, 4096 26.9 / 31.5; 5120 elements: 20.5 / 23.5 at 4096.
 // Rows beyond 8192 have nothing in registers to gain.
 constexpr int RN_WAVES = 4;
 constexpr int RN_AHEAD_PER_CU = 12;

@@ -38,7 +38,7 @@ struct PagedOut {
 // Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles spill 13 registers in front of and behind
 // the loop over the keys, not in it. Of bf16 heads of 128 one has the registers to itself: squeezed into half of them its results and
 // addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26. Of f32 heads of 128 too, and two row tiles spill 28
-// registers all the same, four of them stored in the loop.
+// registers all the same, two of them in the loop too.
 template <typename E, int D>
 constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 

@@ -21,7 +21,7 @@ own = False
 # the 7B and 72B models
 LAYOUTS = {"tiny": (4, 2, 64, "f32", (8, 12, 12)), "7b": (28, 4, 128, "bf16", (16, 24, 24)), "72b": (64, 8, 128, "bf16", (16, 24, 24))}
 THETA = 1e6
-MAX_PAIRS = 1.5e9          # (row, entry) pairs over all query heads of a batch: what the largest listed chunk has
+MAX_PAIRS = 9e8            # (row, entry) pairs over all query heads of a batch: no more than the largest listed chunk has
 MAX_ENTRIES = 1.2e6        # entries times KV heads of a batch
 BLOCK = 16                 # entries that share a scale
 E_MIN, E_MAX = -117, 120   # its exponents

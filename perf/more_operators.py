@@ -353,7 +353,7 @@ def _store(st):
         wide = e.repeat_interleave(BLOCK, 1)
         raw = pool.view(torch.uint8).transpose(1, 2)
         was = raw[old_page, old_slot].view(torch.float8_e4m3fn).float()
-        raw[old_page, old_slot] = _code(was * _pow2(before_e.repeat_interleave(BLOCK, 1)[first] - wide[first])[..., None]).view(torch.uint8)
+        raw[old_page, old_slot] = _code(was * _pow2((before_e.repeat_interleave(BLOCK, 1)[first] - wide[first]).clamp(min=-126))[..., None]).view(torch.uint8)
         raw[new_page, new_slot] = _code(x[new_row] * _pow2(-wide[is_new])[..., None]).view(torch.uint8)
         scale.transpose(1, 2)[block_page[written], block[written]] = _pow2(e[written])
 

@@ -60,8 +60,8 @@ typedef enum { QP_F32 = 0, QP_BF16 = 1 } qp_dtype;
  * 4 exponent bits with bias 7, 3 mantissa bits, no infinities, largest value 448; nearest, ties to even, values
  * beyond +-448 saturate, NaN stays NaN) when qp_topk_compact stores them, and qp_group_attend widens them exactly
  * when it reads them. The group's own K, V (attended to before pruning) and the scores are unaffected.
- * Supported with bf16 layouts of head_dim 128. */
-typedef enum { QP_CACHE_SAME = 0, QP_CACHE_FP8_E4M3 = 1 } qp_cache_format;
+ * Supported with bf16 layouts of head_dim 128. QP_CACHE_FP8_E4M3_SCALED is a format of paged pools only (qp_paged.h). */
+typedef enum { QP_CACHE_SAME = 0, QP_CACHE_FP8_E4M3 = 1, QP_CACHE_FP8_E4M3_SCALED = 2 } qp_cache_format;
 
 /* The three importance functions listed under Eq. 2 (Sec. 3.2). Larger score = kept first. */
 typedef enum {

@@ -7,7 +7,9 @@
  * Here entries live in pages of a pool, a table says which pages a sequence has, and lengths are DEVICE values, so that a
  * captured graph of a decoding step can be replayed while they grow:
  *   qp_paged_append   stores new keys and values (a step's, a chunk's, or what a video left in a flat cache) in the pages
+ *   qp_paged_append_rope    the same with the keys turned by their rotary angles on the way, and the new tokens' queries too
  *   qp_paged_attend   attention of every sequence's new tokens over its entries
+ *   qp_paged_attend_window  the same where a token sees a window of the last entries and the sequence's first ones
  *   qp_paged_weigh    the attention weight that every entry received from those tokens, taken anew or accumulated
  *   qp_paged_evict    keeps the entries of most weight (and the first and the last ones), packed into other pages
  *
@@ -23,6 +25,12 @@
  * qp_paged_attend, and the source of qp_paged_evict. In a call that writes it (append, weigh, the destination of evict)
  * it may be there once: two writers of one entry race, and only its value is then unspecified.
  * Supported: dtype f32 or bf16, head_dim 64 or 128, pages of 16, 32, 64, 128 or 256 tokens; 8-bit pools (E4M3) as in qp.h.
+ *   QP_CACHE_FP8_E4M3_SCALED: an 8-bit pool (bf16 layouts of head_dim 128) whose entries j / 16 of a sequence share a scale per KV head, one
+ * for keys and one for values: an element is code * scale, scale a power of two from 2^-117 to 2^120. E4M3 codes alone hold magnitudes from 2^-9 to
+ * 448: keys of channels with large offsets saturate. Codes are floating-point themselves, so a finer scale would not make them more exact; a power of two
+ * is exact wherever it is applied. An append gives a block the least scale that holds its finite values (infinities saturate, NaN stays) and never
+ * a smaller one than the block's earlier entries have; where it grows, their codes are divided with it, exactly down to 2^-6 of the new
+ * scale and rounded below. qp_paged_weigh and qp_paged_evict do not take such pools (UNSUPPORTED).
  */
 #ifndef QP_PAGED_H_
 #define QP_PAGED_H_
@@ -43,6 +51,8 @@ typedef struct {
   int32_t n_pages;
   int32_t page_tokens; /* 16, 32, 64, 128 or 256                                                               */
   int32_t format;      /* qp_cache_format of k and v                                                           */
+  float* k_scale;      /* [n_pages][n_kv_heads][page_tokens / 16], QP_CACHE_FP8_E4M3_SCALED only: powers of two */
+  float* v_scale;
 } qp_paged_cache;
 
 /* The sequences of a call. Sequence s has the entries 0 .. len[s] - 1, entry j in page page_table[s][j / page_tokens] at
@@ -78,6 +88,27 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
                           const void* v, int64_t token_stride, int64_t head_stride, const int32_t* pos,
                           int64_t pos_token_stride, int64_t pos_head_stride, qp_cache_format source_format, void* hip_stream);
 
+/* Rotary positions of a call's rows. Frequency i of head_dim / 2 is theta^(-2 i / head_dim); the first section[0] of them turn by the position
+ * index on axis 0 (temporal), the next section[1] on axis 1 (height), the last section[2] on axis 2 (width). */
+typedef struct {
+  const int32_t* pos;   /* device: row r's index on axis a at pos[a * axis_stride + r]                        */
+  int64_t axis_stride;  /* 0: the same index on all axes (text)                                               */
+  float theta;
+  int32_t section[3];   /* sum head_dim / 2                                                                   */
+} qp_paged_rope;
+
+/* qp_paged_append of keys that are not rotated yet (a plain projection's): pairs (i, i + head_dim / 2) of every key are turned by
+ * pos * frequency on the way, and so are the queries of the same rows, if given. Angles as exact as f32 holds their sines and cosines,
+ * f32 arithmetic, one rounding, to the pool's type (8-bit codes too) or, queries, the layout's.
+ *   k, v: as in qp_paged_append (token_stride, head_stride in elements; rows of the layout's dtype)
+ *   q_or_null: query head h of row r at q + (r * q_token_stride + h * q_head_stride), 16-byte aligned rows; q_out [n_rows][H_q][d], which
+ *     may be q itself where that is dense. Rows of nobody are left as they were; both NULL: keys and values only
+ *   pos, pos_token_stride, pos_head_stride: the entries' token positions, as in qp_paged_append */
+qp_status qp_paged_append_rope(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch,
+                               const qp_paged_rope* rope, const void* q_or_null, int64_t q_token_stride, int64_t q_head_stride,
+                               const void* k, const void* v, int64_t token_stride, int64_t head_stride, const int32_t* pos,
+                               int64_t pos_token_stride, int64_t pos_head_stride, void* q_out, void* hip_stream);
+
 /* Attention of the new tokens: q, out [n_rows][H_q][d] (layout dtype), lse_or_null [H_q][n_rows] f32 (natural log). A row that
  * sees no entry (the sequence has fewer than its new rows, or none of its pages is there) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (to two bf16 terms in calls of up to
@@ -89,6 +120,14 @@ qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, 
  *     whose partial results (f32) lie there until a second launch merges them; without it (or with less) to fewer. */
 qp_status qp_paged_attend(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, const void* q,
                           void* out, float* lse_or_null, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* qp_paged_attend with a sliding window: the row that is entry p sees the entries j <= p with j > p - window or j < n_sink, so each
+ * new token has a window of its own. window >= 1 entries, the row's own included; n_sink >= 0. What no row sees is not read: pages
+ * between the first entries and the windows may have been given back (-1 in the table). Arguments, arithmetic and workspace otherwise as
+ * qp_paged_attend; a window of max_len entries gives its results (a row's last bits may differ). */
+qp_status qp_paged_attend_window(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, int32_t window,
+                                 int32_t n_sink, const void* q, void* out, float* lse_or_null, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
 
 /* weight[j] of KV head h = (accumulate ? weight[j] : 0) + the sum of exp(scale * q.k_j - lse) over the sequence's new rows that
  * see j and the H_q / H_kv query heads of h, for every entry j < len[s]: with the lse that qp_paged_attend wrote for the same

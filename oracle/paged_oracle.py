@@ -1,9 +1,11 @@
 """fp64 oracle of the paged cache (include/qp_paged.h), written from the definitions, sequence by sequence.
 
 A pool is a dict of numpy arrays k, v [pages][H_kv][P][d], pos, weight [pages][H_kv][P]; a batch is table [S][pages], lens [S],
-row_start [S + 1]. Nothing here shares code with the kernels.
+row_start [S + 1]. A pool with scales has codes in k and v and k_scale, v_scale [pages][H_kv][P / 16]. Nothing here shares code with the kernels.
 """
 import numpy as np
+
+from oracle.qp_oracle import fp8_e4m3_round
 
 
 def places(table, length, page_tokens, n_pages):
@@ -21,8 +23,14 @@ def _sequences(batch, n_rows):
         yield s, length, begin, end - begin
 
 
-def attend(q, pool, batch, scale):
-    """out [rows][H_q][d] and lse [H_q][rows] (NaN where a row belongs to nobody), and per output the softmax mean of |v| and per row the largest |logit| and
+def dequantised(pool):
+    """A pool with scales as one of the values that its codes stand for."""
+    wide = lambda x: np.repeat(x, 16, axis=2)[..., None]
+    return dict(pool, k=pool["k"] * wide(pool["k_scale"]), v=pool["v"] * wide(pool["v_scale"]))
+
+
+def attend(q, pool, batch, scale, window=None, n_sink=0):
+    """A row that is entry p sees j <= p, with a window those with j > p - window or j < n_sink. out [rows][H_q][d] and lse [H_q][rows] (NaN where a row belongs to nobody), and per output the softmax mean of |v| and per row the largest |logit| and
     the largest sum |q||k|, which error bounds need."""
     n_rows, h_q, d = q.shape
     n_pages, h_kv, p, _ = pool["k"].shape
@@ -36,6 +44,8 @@ def attend(q, pool, batch, scale):
             k, v = pool["k"][page, qh // r, slot], pool["v"][page, qh // r, slot]
             for i in range(n):
                 see = j <= base + i
+                if window is not None:
+                    see &= (j > base + i - window) | (j < n_sink)
                 row = begin + i
                 if not see.any():
                     out[row, qh], lse[qh, row] = 0, -np.inf
@@ -105,3 +115,54 @@ def evict(pool, table, lens, keep, n_first, n_last):
             order = sorted(range(len(j)), key=lambda x: (not stays[x], -w[x], j[x]))
             kept.append(np.sort(j[order[:keep]]))
     return kept
+
+
+def turn(x, axes, theta, section):
+    """x [rows][heads][d], pairs (i, i + d / 2) turned by axes[axis(i)][row] * theta^(-2 i / d)."""
+    half = x.shape[-1] // 2
+    axis = np.repeat(np.arange(3), section)
+    angle = np.asarray(axes, np.float64)[axis].T * np.float64(theta) ** (-np.arange(half) / half)
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    lo, hi = x[..., :half], x[..., half:]
+    return np.concatenate([lo * c - hi * s, hi * c + lo * s], -1)
+
+
+def block_exponent(x, largest):
+    """The least e from -117 to 120 with |x| <= largest * 2^e for the finite ones of x."""
+    most = max([0.0] + [abs(float(v)) for v in np.ravel(x) if np.isfinite(v)])
+    e = -117
+    while e < 120 and most > largest * 2.0 ** e:
+        e += 1
+    return e
+
+
+def append_scaled(k, v, k_size, pos, pool, batch, k_largest, store=fp8_e4m3_round):
+    """The pool with scales after the new rows: entry by entry, which gives a block the same scale as all at once, and its earlier entries'
+    codes as if the block's scale had been known (one rescaling of what was there before the call). k_size: rows whose magnitudes the keys' scales
+    hold, up to k_largest; store: codes of scaled values."""
+    pool = {name: x.copy() for name, x in pool.items()}
+    n_pages, h_kv, p, _ = pool["k"].shape
+    for s, length, begin, n in _sequences(batch, len(k)):
+        length = max(0, min(length, len(batch["table"][s]) * p))
+        first = length - n
+        for block in range(max(first, 0) // 16, -(-length // 16)):
+            page, at = batch["table"][s][block * 16 // p], block * 16 % p
+            if not 0 <= page < n_pages or n == 0:
+                continue
+            new = [j for j in range(block * 16, min(length, block * 16 + 16)) if j >= first]
+            old = [j for j in range(block * 16, min(first, block * 16 + 16))]
+            rows = [begin + j - first for j in new]
+            for h in range(h_kv):
+                for x, size, name, largest in ((k, k_size, "k", k_largest), (v, v, "v", 448.0)):
+                    e = block_exponent(size[rows, h], largest)
+                    scale = pool[name + "_scale"]
+                    if old:
+                        was = int(np.log2(scale[page, h, at // 16]))
+                        e = max(e, was)
+                        slots = [j % p for j in old]
+                        pool[name][page, h, slots] = fp8_e4m3_round(pool[name][page, h, slots] * 2.0 ** (was - e))
+                    scale[page, h, at // 16] = 2.0 ** e
+                    pool[name][page, h, [j % p for j in new]] = store(x[rows, h] * 2.0 ** -e)
+            for j, row in zip(new, rows):
+                pool["pos"][page, :, j % p], pool["weight"][page, :, j % p] = pos[row], 0
+    return pool

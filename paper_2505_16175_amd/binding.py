@@ -35,7 +35,7 @@ class qp_cache(ctypes.Structure):
                 ("capacity", ctypes.c_int32), ("len", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
-QP_CACHE_SAME, QP_CACHE_FP8_E4M3 = 0, 1
+QP_CACHE_SAME, QP_CACHE_FP8_E4M3, QP_CACHE_FP8_E4M3_SCALED = 0, 1, 2
 
 
 class qp_attend_plan_info(ctypes.Structure):
@@ -56,7 +56,12 @@ class qp_layer_weights(ctypes.Structure):
 
 class qp_paged_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p),
-                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("format", ctypes.c_int32)]
+                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class qp_paged_rope(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("axis_stride", ctypes.c_int64), ("theta", ctypes.c_float), ("section", ctypes.c_int32 * 3)]
 
 
 class qp_paged_batch(ctypes.Structure):
@@ -95,7 +100,7 @@ class QPError(RuntimeError):
 _lib = None
 _vp, _i32, _i64, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 _LP, _CP = ctypes.POINTER(qp_layout), ctypes.POINTER(qp_cache)
-_PC, _PB = ctypes.POINTER(qp_paged_cache), ctypes.POINTER(qp_paged_batch)
+_PC, _PB, _PR = ctypes.POINTER(qp_paged_cache), ctypes.POINTER(qp_paged_batch), ctypes.POINTER(qp_paged_rope)
 _SP, _WP, _f32 = ctypes.POINTER(qp_layer_shape), ctypes.POINTER(qp_layer_weights), ctypes.c_float
 
 SIGNATURES = {
@@ -131,7 +136,9 @@ SIGNATURES = {
     # include/qp_paged.h
     "qp_paged_workspace_bytes": (_sz, [_LP, _i32, _i32, _i32, _i32, _i32]),
     "qp_paged_append": (_i32, [_LP, _PC, _PB, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _vp]),
+    "qp_paged_append_rope": (_i32, [_LP, _PC, _PB, _PR, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]),
     "qp_paged_attend": (_i32, [_LP, _PC, _PB, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "qp_paged_attend_window": (_i32, [_LP, _PC, _PB, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "qp_paged_weigh": (_i32, [_LP, _PC, _PB, _vp, _vp, _i32, _vp, _sz, _vp]),
     "qp_paged_evict": (_i32, [_LP, _PC, _PB, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
     "qp_paged_plan": (_i32, [_LP, _PC, _PB, _sz, ctypes.POINTER(qp_paged_plan_info)]),
@@ -522,25 +529,33 @@ class PagedCache:
     """Owner of the device buffers behind a qp_paged_cache: a pool of pages that many sequences share."""
 
     def __init__(self, layout: qp_layout, n_pages: int, page_tokens: int, device="cuda", fmt=QP_CACHE_SAME, weights=True,
-                 k=None, v=None, pos=None, weight=None):
-        """New zeroed buffers (positions -1), or the caller's own: k, v [n_pages][H_kv][page_tokens][d] in the layout's dtype
-        or torch.float8_e4m3fn, pos int32 and weight float32 [n_pages][H_kv][page_tokens]. weights=False: a pool without them,
+                 k=None, v=None, pos=None, weight=None, k_scale=None, v_scale=None):
+        """New zeroed buffers (positions -1, scales 1), or the caller's own: k, v [n_pages][H_kv][page_tokens][d] in the layout's
+        dtype or torch.float8_e4m3fn, pos int32 and weight float32 [n_pages][H_kv][page_tokens], with fmt =
+        QP_CACHE_FP8_E4M3_SCALED k_scale, v_scale float32 [n_pages][H_kv][page_tokens / 16]. weights=False: a pool without them,
         which paged_weigh and paged_evict refuse."""
         rows = (n_pages, layout.n_kv_heads, page_tokens)
-        if k is not None and k.dtype == torch.float8_e4m3fn:
+        blocks = (*rows[:2], page_tokens // 16)
+        if k is not None and k.dtype == torch.float8_e4m3fn and fmt == QP_CACHE_SAME:
             fmt = QP_CACHE_FP8_E4M3
-        dt = torch.float8_e4m3fn if fmt == QP_CACHE_FP8_E4M3 else _layout_dtype(layout)
+        scaled = fmt == QP_CACHE_FP8_E4M3_SCALED
+        if not scaled and (k_scale is not None or v_scale is not None):
+            raise ValueError("k_scale, v_scale: expected with QP_CACHE_FP8_E4M3_SCALED only")
+        dt = torch.float8_e4m3fn if scaled or fmt == QP_CACHE_FP8_E4M3 else _layout_dtype(layout)
         self.k = torch.zeros(*rows, layout.head_dim, dtype=dt, device=device) if k is None else k
         self.v = torch.zeros(*rows, layout.head_dim, dtype=dt, device=device) if v is None else v
         self.pos = torch.full(rows, -1, dtype=torch.int32, device=device) if pos is None else pos
         self.weight = torch.zeros(rows, dtype=torch.float32, device=device) if weights and weight is None else weight
+        self.k_scale = torch.ones(blocks, dtype=torch.float32, device=device) if scaled and k_scale is None else k_scale
+        self.v_scale = torch.ones(blocks, dtype=torch.float32, device=device) if scaled and v_scale is None else v_scale
         here = self.k.get_device()
         at = [_dense(t, d, (*rows, layout.head_dim) if t is self.k or t is self.v else rows, name, here)
               for t, d, name in ((self.k, dt, "k"), (self.v, dt, "v"), (self.pos, torch.int32, "pos"))]
         at.append(None if self.weight is None else _dense(self.weight, torch.float32, rows, "weight", here))
+        scales = [_dense(t, torch.float32, blocks, name, here) for t, name in ((self.k_scale, "k_scale"), (self.v_scale, "v_scale"))] if scaled else [None, None]
         self.device_index = here
         self.made_for = (layout.n_kv_heads, layout.head_dim, layout.dtype)
-        self.c = qp_paged_cache(*at, n_pages, page_tokens, fmt)
+        self.c = qp_paged_cache(*at, n_pages, page_tokens, fmt, *scales)
         self.ref = ctypes.byref(self.c)
 
 
@@ -627,6 +642,68 @@ def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
     _check(st, "qp_paged_append")
 
 
+def _row_strides(stride, shape):
+    """(token, head) strides of rows in one run; of one token or head any stride does."""
+    n, h, _ = shape
+    if n == 1 or h == 1:
+        return 0 if n == 1 else stride[0], 0 if h == 1 else stride[1], stride[2]
+    return stride
+
+
+def _kv_strides(k, v, pos, shape, here):
+    sk, sv = _row_strides(k.stride(), shape), _row_strides(v.stride(), shape)
+    if sk != sv or sk[2] != 1:
+        raise ValueError("k and v: expected the same strides and rows in one run")
+    if pos.dtype is not torch.int32 or pos.shape != shape[:1] and pos.shape != shape[:2]:
+        raise ValueError("pos: expected int32 [n_rows] or [n_rows][H_kv]")
+    if k.get_device() != here or v.get_device() != here or pos.get_device() != here:
+        raise ValueError("expected tensors of the current GPU")
+    sp = pos.stride()
+    return sk, (sp[0], sp[1] if len(sp) == 2 else 0)
+
+
+class PagedRope:
+    """Rotary positions of a call's rows: axes int32 [3][n_rows] (temporal, height and width index) or [n_rows] (the same on all), and how
+    many of the head_dim / 2 frequencies turn by each axis. The values may change between calls, and between replays of a captured one."""
+
+    def __init__(self, layout: qp_layout, axes, theta=1e6, section=None):
+        half = layout.head_dim // 2
+        section = (half, 0, 0) if section is None else tuple(section)
+        if axes.dtype is not torch.int32 or axes.dim() not in (1, 2) or axes.dim() == 2 and axes.shape[0] != 3:
+            raise ValueError("axes: expected int32 [3][n_rows] or [n_rows]")
+        if axes.get_device() < 0 or not axes.is_contiguous():
+            raise ValueError("axes: expected a contiguous tensor on the GPU")
+        self.axes, self.n_rows, self.device_index = axes, axes.shape[-1], axes.get_device()
+        self.c = qp_paged_rope(axes.data_ptr(), axes.shape[1] if axes.dim() == 2 else 0, theta, (ctypes.c_int32 * 3)(*section))
+        self.ref = ctypes.byref(self.c)
+
+
+def paged_append_rope(layout, cache: PagedCache, batch: PagedBatch, k, v, pos, rope: PagedRope, q=None, q_out=None):
+    """paged_append of keys that are not rotated yet: k (and q [n_rows][H_q][d] of any strides whose rows are runs, into q_out, dense) turned
+    by their rows' angles on the way. k, v, pos as in paged_append, in the layout's dtype."""
+    here = _same_gpu(layout, cache, batch)
+    n, d, dt = batch.n_rows, layout.head_dim, _layout_dtype(layout)
+    shape = (n, layout.n_kv_heads, d)
+    if k.dtype is not dt or v.dtype is not dt or k.shape != shape or v.shape != shape:
+        raise ValueError(f"k and v: expected {dt} {shape}, got {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
+    sk, sp = _kv_strides(k, v, pos, shape, here)
+    if rope.n_rows != n or rope.device_index != here:
+        raise ValueError("rope: expected positions of the batch's rows on the current GPU")
+    if (q is None) != (q_out is None):
+        raise ValueError("expected q and q_out, or neither")
+    sq, q_at, out_at = (0, 0, 1), None, None
+    if q is not None:
+        shape = (n, layout.n_q_heads, d)
+        if q.dtype is not dt or q.shape != shape or q.get_device() != here:
+            raise ValueError(f"q: expected {dt} {shape} on the current GPU, got {q.dtype} {tuple(q.shape)}")
+        sq, q_at, out_at = _row_strides(q.stride(), shape), q.data_ptr(), _dense(q_out, dt, shape, "q_out", here)
+        if sq[2] != 1:
+            raise ValueError("q: expected rows in one run")
+    st = lib().qp_paged_append_rope(ctypes.byref(layout), cache.ref, batch.of(cache), rope.ref, q_at, sq[0], sq[1], k.data_ptr(), v.data_ptr(),
+                                    sk[0], sk[1], pos.data_ptr(), sp[0], sp[1], out_at, _stream())
+    _check(st, "qp_paged_append_rope")
+
+
 def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None, workspace=None):
     """q, out [n_rows][H_q][d], lse float32 [H_q][n_rows]."""
     here = _same_gpu(layout, cache, batch)
@@ -636,6 +713,17 @@ def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None,
                                _dense(out, dt, shape, "out", here),
                                None if lse is None else _dense(lse, torch.float32, (shape[1], shape[0]), "lse", here), wp, wb, _stream())
     _check(st, "qp_paged_attend")
+
+
+def paged_attend_window(layout, cache: PagedCache, batch: PagedBatch, window, n_sink, q, out, lse=None, workspace=None):
+    """paged_attend in which the row that is entry p sees the entries j <= p with j > p - window or j < n_sink."""
+    here = _same_gpu(layout, cache, batch)
+    dt, shape = _layout_dtype(layout), (batch.n_rows, layout.n_q_heads, layout.head_dim)
+    wp, wb = _scratch(workspace, here)
+    st = lib().qp_paged_attend_window(ctypes.byref(layout), cache.ref, batch.of(cache), window, n_sink, _dense(q, dt, shape, "q", here),
+                                      _dense(out, dt, shape, "out", here),
+                                      None if lse is None else _dense(lse, torch.float32, (shape[1], shape[0]), "lse", here), wp, wb, _stream())
+    _check(st, "qp_paged_attend_window")
 
 
 def paged_weigh(layout, cache: PagedCache, batch: PagedBatch, q, lse, accumulate=True, workspace=None):

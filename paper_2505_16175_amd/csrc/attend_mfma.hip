@@ -138,14 +138,15 @@ __device__ __forceinline__ f32x4 add_four(const bf16x8& p, int hi, f32x4 sum) {
 
 struct Pieces {
   uint2 p[4];
+  float scale[2];  // of K's and V's
 };
-// 8 E4M3 bytes -> 8 bf16 (exact)
-__device__ __forceinline__ u32x4 widen8(uint2 p) {
+// 8 E4M3 bytes, times a power of two, -> 8 bf16 (exact)
+__device__ __forceinline__ u32x4 widen8(uint2 p, float scale = 1.f) {
   u32x4 o;
-  o.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.x, 1.f, false));
-  o.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.x, 1.f, true));
-  o.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.y, 1.f, false));
-  o.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.y, 1.f, true));
+  o.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.x, scale, false));
+  o.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.x, scale, true));
+  o.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.y, scale, false));
+  o.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(p.y, scale, true));
   return o;
 }
 
@@ -159,15 +160,29 @@ struct PagedTileArgs : AttendArgs {
   int row_blocks;  // of 256 stacked rows, for max_new tokens
   int chunk;       // filled per workgroup
 };
+// The same over a pool whose blocks of 16 entries have scales, and where a row sees a window of entries and the sequence's first ones: a row
+// block then leaves out the tiles between the two (RowsGap), and counts tiles without them.
+template <bool SCALED, bool WINDOW>
+struct PagedTileArgsOf : PagedTileArgs {
+  int span;  // keys in a row block's own count that a sequence has at most
+};
+template <class Args>
+struct PagedTileKind {
+  static constexpr bool PAGED = std::is_same_v<Args, PagedTileArgs>, SCALED = false, WINDOW = false;
+};
+template <bool S, bool W>
+struct PagedTileKind<PagedTileArgsOf<S, W>> {
+  static constexpr bool PAGED = true, SCALED = S, WINDOW = W;
+};
 __device__ unsigned char paged_zeros[8 * 256];  // eight rows of a missing page
 
 // A wavefront's 32 rows of a chunk (or of the whole): partial results, or the output. Where a result is not finite, a value that
 // some of its rows do not see may have reached them (0 times infinity): such rows are done again, 16 at a time, by the arithmetic
 // for few rows, which keeps those apart.
-template <bool F8>
+template <bool F8, bool SCALED, bool WINDOW>
 __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const PagedSeq& seq, int seq_no, int h, int chunk, unsigned char* smem,
-                                             int wave, bool wave_live, int row0, int n_rows, int key_begin, int key_end, float m_run,
-                                             float l_run, f32x16 (&o)[4]) {
+                                             int wave, bool wave_live, int row0, int n_rows, int key_begin, int key_end, const RowsGap& gap,
+                                             float m_run, float l_run, f32x16 (&o)[4]) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int r_heads = a.h_q / a.h_kv;
   const size_t total = (size_t)a.pg.n_rows * a.h_q;
@@ -191,18 +206,20 @@ __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const Paged
 #pragma unroll
     for (int r = 0; r < 16; ++r) bad = bad || pr_not_finite(o[n][r]);
   if (__any(bad)) {
-    using E = std::conditional_t<F8, uint8_t, bf16_t>;
+    using E = std::conditional_t<SCALED, ScaledCode, std::conditional_t<F8, uint8_t, bf16_t>>;
     for (int half = 0; half < 32 && row0 + half < n_rows; half += 16) {
-      RowsWave<E, MF_D, 1> rows;
+      RowsWave<E, MF_D, 1, WINDOW> rows;
       const int count = min(16, n_rows - row0 - half);
       rows.init(a.pg, seq, a.q, h, row0 + half, count);
-      const int end = min(key_end, min(seq.len, seq.base + (row0 + half + count - 1) / r_heads + 1));
+      const int entries = min(seq.len, seq.base + (row0 + half + count - 1) / r_heads + 1);
+      const int end = min(key_end, WINDOW ? entries - gap.gap : entries);
       for (int key = key_begin; key < end; key += RowsLayout<E, MF_D>::BK) {
         RowsBlock<E, MF_D> b;
-        rows.load(b, a.pg, h, key, end, [&](int k) {
+        const int at = WINDOW ? gap.entry(key) : key, at_end = WINDOW ? entries : end;
+        rows.load(b, a.pg, h, at, at_end, [&](int k) {
           return __builtin_amdgcn_readfirstlane(a.pg.table[(size_t)seq_no * a.pg.table_pages + (k >> a.pg.page_shift)]);
         });
-        rows.compute(b, key, end, a.scale_log2);
+        rows.template compute<true>(b, at, at_end, a.scale_log2, a.pg.window, a.pg.n_sink);
       }
       const float den = rows.denominator(0);
       const bool none = den == 0.f;
@@ -291,7 +308,7 @@ __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const Paged
 // which is their own rounding.
 template <bool F8, class Args>
 __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
-  constexpr bool PAGED = std::is_same_v<Args, PagedTileArgs>;
+  constexpr bool PAGED = PagedTileKind<Args>::PAGED, SCALED = PagedTileKind<Args>::SCALED, WINDOW = PagedTileKind<Args>::WINDOW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // wave-uniform for the compiler too: scalar address and branch work
@@ -324,7 +341,9 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     if (a.chunk >= a.n_split) return;
     seq = paged_seq_of(a.pg, seq_no);
     a.n_g = seq.n;
-    if (a.chunk > 0 && a.chunk * a.split_tiles >= (seq.len + MF_BN - 1) / MF_BN) return;  // chunk 0 always answers
+    int tiles = (seq.len + MF_BN - 1) / MF_BN;
+    if constexpr (WINDOW) tiles = (min(seq.len, a.span) + MF_BN - 1) / MF_BN;
+    if (a.chunk > 0 && a.chunk * a.split_tiles >= tiles) return;  // chunk 0 always answers
   }
   const int base = PAGED ? seq.base : 0;  // PAGED: entries before the new tokens
   int n_rows = a.n_g * r_heads;
@@ -415,7 +434,12 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   const int t_wg_max = min(hb_late * MF_HB + MF_HB - 1, n_rows - 1) / r_heads;
   const bool wave_live = row0 < n_rows && !unpaired;
   const int n_ct = PAGED ? 0 : (a.c + MF_BN - 1) / MF_BN;  // cache tiles
-  const int n_tiles = PAGED ? max(0, base + t_wg_max + MF_BN) / MF_BN : n_ct + t_wg_max / MF_BN + 1;  // + group tiles
+  // WINDOW: tile numbers from here on are the row block's own, real() gives those of the sequence
+  RowsGap gap{0, 0};
+  if constexpr (WINDOW) gap = rows_gap(a.pg.window, a.pg.n_sink, base + hb_early * MF_HB / r_heads, MF_BN);
+  const int gap_tiles = gap.gap / MF_BN;
+  auto real = [&](int tile) { return WINDOW ? tile + (tile * MF_BN < gap.jump ? 0 : gap_tiles) : tile; };
+  const int n_tiles = PAGED ? max(0, base + t_wg_max + MF_BN) / MF_BN - gap_tiles : n_ct + t_wg_max / MF_BN + 1;  // + group tiles
   // key split: a chunk walks cache tiles [t_begin, t_end); the last chunk goes on through the group tiles
   const int t_begin = chunk * a.split_tiles;
   const int t_end = PAGED ? min(n_tiles, t_begin + a.split_tiles) : chunk == my_split - 1 ? n_tiles : t_begin + a.split_tiles;
@@ -443,6 +467,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     const unsigned char* src;
     unsigned o0, o1, step;
     int tile, event;
+    const float* scale;  // SCALED: of the wavefront's eight keys
   };
   // PAGED: the page numbers of the table's entries from list_first on, one per lane, and which of them are there; what is missing
   // of the tiles under way, four bits (16 keys each) at 4 * (tile & 7); the eight keys of this wavefront in K's next tile
@@ -455,9 +480,9 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     bool ok;
   };
   const int last_key = seq.len - 1;
-  auto eight_keys = [&](int tile) {
+  auto eight_keys = [&](int own_tile) {
     if constexpr (PAGED) {
-      const int shift = a.pg.page_shift, tile_page = (tile * MF_BN) >> shift;
+      const int tile = real(own_tile), shift = a.pg.page_shift, tile_page = (tile * MF_BN) >> shift;
       if (tile_page + 3 - list_first >= 64 || tile_page < list_first || list_ok == 0) {
         list_first = tile_page;
         list = -1;
@@ -468,7 +493,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
       unsigned out = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) out |= (list_ok >> (((tile * MF_BN + 16 * i) >> shift) - list_first)) & 1 ? 0u : 1u << i;
-      const int sl = 4 * (tile & 7);
+      const int sl = 4 * (own_tile & 7);
       missing = (missing & ~(15u << sl)) | (out << sl);
       const int key = min(tile * MF_BN + 8 * wave, last_key & ~7);
       const int page = __builtin_amdgcn_readlane(list, (key >> shift) - list_first);
@@ -479,8 +504,11 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     }
   };
   Eight k_keys{};
-  auto place = [&](Stream& s, const unsigned char* pool, const Eight& e, unsigned c0, unsigned c1) {
+  const float *k_scales = nullptr, *v_scales = nullptr;
+  if constexpr (SCALED) k_scales = a.pg.k_scale, v_scales = a.pg.v_scale;
+  auto place = [&](Stream& s, const unsigned char* pool, const float* scales, const Eight& e, unsigned c0, unsigned c1) {
     if constexpr (PAGED) {
+      if constexpr (SCALED) s.scale = scales + e.at / (16 * CROW);
       s.src = e.ok ? pool + e.at : (const unsigned char*)paged_zeros;
       const int sub = lane >> 4;  // keys past the last one repeat it: masked, never used
       s.o0 = (unsigned)min(sub, e.left) * CROW + (c0 >> (F8 ? 1 : 0));
@@ -510,10 +538,10 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   sk.tile = sv.tile = t_begin;
   if constexpr (PAGED) {
     if (t_begin < t_end) {
-      list_first = (t_begin * MF_BN) >> a.pg.page_shift;
+      list_first = (real(t_begin) * MF_BN) >> a.pg.page_shift;
       k_keys = eight_keys(t_begin);
-      place(sk, ck, k_keys, st_kc0, st_kc1);
-      place(sv, cv, k_keys, st_vc0, st_vc1);
+      place(sk, ck, k_scales, k_keys, st_kc0, st_kc1);
+      place(sv, cv, v_scales, k_keys, st_vc0, st_vc1);
     }
   } else {
     settle(sk, ck, gk, st_kc0, st_kc1);
@@ -524,7 +552,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     if constexpr (PAGED) {
       if (++sk.tile < t_end) {
         k_keys = eight_keys(sk.tile);
-        place(sk, ck, k_keys, st_kc0, st_kc1);
+        place(sk, ck, k_scales, k_keys, st_kc0, st_kc1);
       }
     } else {
       advance(sk, ck, gk, st_kc0, st_kc1);
@@ -533,17 +561,24 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   const int cache_end = PAGED ? t_end : n_ct;  // tiles of an 8-bit cache
   // A pair's four requests: halves of its K tile (0, 1) and of its V tile (2, 3). Tiles of an 8-bit cache cannot go to LDS
   // directly: this lane's 8 bytes of each half are pending in registers until they are stored, widened.
+  // SCALED: their scale comes with a pair's second half, when the first is stored; it is loaded like them, since a scalar load would be
+  // waited for together with all LDS reads under way.
   Pieces pend;
+  unsigned nought = 0;
+  if constexpr (SCALED) asm("" : "+v"(nought));
   auto load_piece = [&](int i) {
     const Stream& s = i < 2 ? sk : sv;
+    if constexpr (SCALED) {
+      if (i & 1) pend.scale[i >> 1] = s.scale[nought];
+    }
     return *(const uint2*)(s.src + ((i & 1) ? s.o1 : s.o0));
   };
   auto request_half = [&](int i, unsigned dst) {  // dst: LDS address of the slot's K tile
     const Stream& s = i < 2 ? sk : sv;
     lds_dma16_to(s.src, (i & 1) ? s.o1 : s.o0, dst + (i < 2 ? 0 : MF_V0) + (i & 1) * 1024);
   };
-  auto store_piece = [&](int i, uint2 p, int slot) {
-    *(u32x4*)(smem + slot * MF_TILE + (i < 2 ? 0 : MF_V0) + (i & 1) * 1024 + wave * 2048 + lane * 16) = widen8(p);
+  auto store_piece = [&](int i, uint2 p, float scale, int slot) {
+    *(u32x4*)(smem + slot * MF_TILE + (i < 2 ? 0 : MF_V0) + (i & 1) * 1024 + wave * 2048 + lane * 16) = widen8(p, SCALED ? scale : 1.f);
   };
   auto request_k = [&](int slot) {
     if (F8 && sk.tile < cache_end) pend.p[0] = load_piece(0), pend.p[1] = load_piece(1);
@@ -554,10 +589,10 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
     else request_half(2, st_lds + slot * MF_TILE), request_half(3, st_lds + slot * MF_TILE);
   };
   auto store_k = [&](int tile, const Pieces& p, int slot) {  // if `tile` is a tile of an 8-bit cache
-    if (F8 && tile < cache_end) store_piece(0, p.p[0], slot), store_piece(1, p.p[1], slot);
+    if (F8 && tile < cache_end) store_piece(0, p.p[0], p.scale[0], slot), store_piece(1, p.p[1], p.scale[0], slot);
   };
   auto store_v = [&](int tile, const Pieces& p, int slot) {
-    if (F8 && tile < cache_end) store_piece(2, p.p[2], slot), store_piece(3, p.p[3], slot);
+    if (F8 && tile < cache_end) store_piece(2, p.p[2], p.scale[1], slot), store_piece(3, p.p[3], p.scale[1], slot);
   };
 
   // fragment read addresses (bytes inside a tile)
@@ -703,7 +738,9 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   // it - 1, which every wavefront has left, is free. Each pair is 4 requests per wavefront (the last one 2).
   auto turn = [&](int it) {
     if (it + 1 >= n) return;
-    if (it + 3 < n) __builtin_amdgcn_s_waitcnt(MF_VMCNT4);
+    // SCALED: six loads of a pair are under way, none of them to LDS, and the compiler waits for them
+    if (SCALED) {
+    } else if (it + 3 < n) __builtin_amdgcn_s_waitcnt(MF_VMCNT4);
     else __builtin_amdgcn_s_waitcnt(MF_VMCNT0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -719,7 +756,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   auto advance_both = [&]() {
     if constexpr (PAGED) {
       ++sv.tile;
-      place(sv, cv, k_keys, st_vc0, st_vc1);
+      place(sv, cv, v_scales, k_keys, st_vc0, st_vc1);
       advance_k();
     } else {
       advance(sk, ck, gk, st_kc0, st_kc1);
@@ -736,12 +773,22 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   // Masked tiles: the cache's last one if cut off, and the group's from this wavefront's diagonal on.
   const int diag_tile = PAGED ? max(0, base + t_w_min + 1) / MF_BN : n_ct + (t_w_min + 1) / MF_BN;  // first with keys beyond t_w_min
   auto masked = [&](int tile) {
+    if constexpr (WINDOW) {  // also where the last row's window begins behind the tile's first key
+      const int t = real(tile);
+      return t >= diag_tile || ((missing >> (4 * (tile & 7))) & 15u) != 0 || (t * MF_BN <= base + t_w_max - a.pg.window && (t + 1) * MF_BN > a.pg.n_sink);
+    }
     if constexpr (PAGED) return tile >= diag_tile || ((missing >> (4 * (tile & 7))) & 15u) != 0;
     else return tile == cache_tail || tile >= diag_tile;
   };
   auto mask = [&](f32x16& st, int tile, int kb) {
     if constexpr (PAGED) {
-      mask_block(st, base + t_lane - tile * MF_BN - 32 * kb - 4 * g);
+      const int lim = base + t_lane - real(tile) * MF_BN - 32 * kb - 4 * g;
+      mask_block(st, lim);
+      if constexpr (WINDOW) {
+        const int low = lim - a.pg.window, sinks = a.pg.n_sink - real(tile) * MF_BN - 32 * kb - 4 * g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[r] = 8 * (r >> 2) + (r & 3) <= low && 8 * (r >> 2) + (r & 3) >= sinks ? -INFINITY : st[r];
+      }
       const unsigned out = missing >> (4 * (tile & 7) + 2 * kb);
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] = (out >> (r >> 3)) & 1 ? -INFINITY : st[r];
@@ -752,7 +799,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   };
   const bool late = my_split > 1 && a.split_tiles > 2;  // the second and third pair are requested behind the first wait
   // this wavefront's last tile (relative; -1: no rows)
-  const int last = !wave_live ? -1 : PAGED ? max(0, min(n, max(0, base + t_w_max + MF_BN) / MF_BN - t_begin)) - 1
+  const int last = !wave_live ? -1 : PAGED ? max(0, min(n, max(0, base + t_w_max + MF_BN) / MF_BN - gap_tiles - t_begin)) - 1
                                            : min(n, n_ct + t_w_max / MF_BN + 1 - t_begin) - 1;
 
 #pragma unroll
@@ -830,7 +877,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
       const unsigned turn_mask = (it & 1) ? 3 * MF_TILE : MF_TILE;  // slot it & 3 -> slot (it + 1) & 3
       step(true_type(), false_type(), sa, sb, pa, pb, 0u, false, [&](int s) {
         if (F8 && (s & 1)) {
-          store_piece(s >> 1, pend.p[s >> 1], (it + 2) & 3);
+          store_piece(s >> 1, pend.p[s >> 1], pend.scale[s >> 2], (it + 2) & 3);
           pend.p[s >> 1] = load_piece(s >> 1);
         }
       });
@@ -870,7 +917,8 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   }
 
   if constexpr (PAGED) {
-    paged_finish<F8>(a, seq, seq_no, h, chunk, smem, wave, wave_live, row0, n_rows, t_begin * MF_BN, t_end * MF_BN, m_run, l_run, o);
+    paged_finish<F8, SCALED, WINDOW>(a, seq, seq_no, h, chunk, smem, wave, wave_live, row0, n_rows, t_begin * MF_BN, t_end * MF_BN, gap, m_run,
+                                     l_run, o);
     return;
   }
   if (my_split > 1) {
@@ -1150,7 +1198,9 @@ static void set_lds_limit() {
   const int dev = current_device();
   if (dev >= 0 && attr_set[dev]) return;
   for (const void* f : {(const void*)attend_mfma_kernel<false, AttendArgs>, (const void*)attend_mfma_kernel<true, AttendArgs>,
-                        (const void*)attend_mfma_kernel<false, PagedTileArgs>, (const void*)attend_mfma_kernel<true, PagedTileArgs>})
+                        (const void*)attend_mfma_kernel<false, PagedTileArgs>, (const void*)attend_mfma_kernel<true, PagedTileArgs>,
+                        (const void*)attend_mfma_kernel<true, PagedTileArgsOf<true, false>>, (const void*)attend_mfma_kernel<false, PagedTileArgsOf<false, true>>,
+                        (const void*)attend_mfma_kernel<true, PagedTileArgsOf<false, true>>, (const void*)attend_mfma_kernel<true, PagedTileArgsOf<true, true>>})
     (void)hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, MF_LDS);
   if (dev >= 0) attr_set[dev] = true;
 }
@@ -1208,6 +1258,14 @@ long long paged_tile_blocks(const PagedArgs& a, const PagedPlan& p) {
   return units * a.h_kv * p.tiles;
 }
 
+template <bool F8, bool SCALED, bool WINDOW>
+static void launch_tiles_of(const PagedTileArgs& a, int span, dim3 grid, hipStream_t s) {
+  PagedTileArgsOf<SCALED, WINDOW> of{};
+  (PagedTileArgs&)of = a;
+  of.span = span;
+  hipLaunchKernelGGL((attend_mfma_kernel<F8, PagedTileArgsOf<SCALED, WINDOW>>), grid, dim3(MF_NT), MF_LDS, s, of);
+}
+
 void launch_paged_tiles(const PagedArgs& pg, const PagedPlan& p, const void* q, void* out, float* lse, float* part_o, float* part_lse,
                         hipStream_t s) {
   set_lds_limit();
@@ -1219,8 +1277,18 @@ void launch_paged_tiles(const PagedArgs& pg, const PagedPlan& p, const void* q, 
   a.part_o = part_o, a.part_lse = part_lse;
   a.pg = pg, a.row_blocks = p.tiles;
   const dim3 grid((unsigned)p.workgroups);
-  if (pg.fp8) hipLaunchKernelGGL((attend_mfma_kernel<true, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
-  else hipLaunchKernelGGL((attend_mfma_kernel<false, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
+  const bool scaled = pg.fp8 == QP_CACHE_FP8_E4M3_SCALED;
+  if (pg.window > 0) {
+    if (scaled) launch_tiles_of<true, true, true>(a, p.span, grid, s);
+    else if (pg.fp8) launch_tiles_of<true, false, true>(a, p.span, grid, s);
+    else launch_tiles_of<false, false, true>(a, p.span, grid, s);
+  } else if (scaled) {
+    launch_tiles_of<true, true, false>(a, p.span, grid, s);
+  } else if (pg.fp8) {
+    hipLaunchKernelGGL((attend_mfma_kernel<true, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
+  } else {
+    hipLaunchKernelGGL((attend_mfma_kernel<false, PagedTileArgs>), grid, dim3(MF_NT), MF_LDS, s, a);
+  }
 }
 
 void launch_attend_merge(const AttendArgs& a, hipStream_t s) {

@@ -6,6 +6,10 @@
 
 namespace qp {
 
+constexpr int PAGED_BLOCK = 16;  // entries that share a scale
+// Exponents of the scales: from the least whose smallest code is a normal f32 and bf16 value to the least that holds the largest f32.
+constexpr int PAGED_SCALE_MIN = -117, PAGED_SCALE_MAX = 120;
+
 struct PagedArgs {
   void* k;         // [n_pages][h_kv][1 << page_shift][d]
   void* v;
@@ -15,10 +19,13 @@ struct PagedArgs {
   const int32_t* len;        // [n_seqs]
   const int32_t* row_start;  // [n_seqs + 1]
   int n_pages, page_shift;
-  int fp8;         // 1: the pool holds one E4M3 byte per element
+  int fp8;         // qp_cache_format of the pool: not 0: it holds one E4M3 byte per element
+  float* k_scale;  // [n_pages][h_kv][entries / PAGED_BLOCK], pools with scales only: powers of two
+  float* v_scale;
   int n_seqs, table_pages, n_rows, max_new, max_len;
   int h_q, h_kv;
   float scale_log2;  // softmax scale * log2(e)
+  int window, n_sink;  // window > 0: the row that is entry p sees j > p - window and j < n_sink only; 0: all up to itself
 };
 
 // One sequence of a batch: row i of its n new ones (from row0) sees the entries j <= base + i, j < len.
@@ -44,6 +51,24 @@ __host__ __device__ inline size_t paged_row(int page, int h, int slot, int h_kv,
   return (((size_t)page * h_kv + h) << page_shift) + slot;
 }
 
+// Entries that a window leaves out between the first ones and a row tile's windows: the tile's keys, in its own count, are those below `jump`
+// and then those from jump + gap on. Both are whole blocks of keys, which the kernels never read across.
+struct RowsGap {
+  int jump, gap;
+  __host__ __device__ inline int entry(int key) const { return key < jump ? key : key + gap; }
+};
+// Of rows whose first one is entry `first` (-2^30 and up): blocks of `step` keys. window, n_sink <= 2^30.
+__host__ __device__ inline RowsGap rows_gap(int window, int n_sink, int first, int step) {
+  const int low = first - window + 1 > 0 ? first - window + 1 : 0;  // what the windows begin with
+  const int jump = ((n_sink < low ? n_sink : low) + step - 1) / step * step, gap = low / step * step - jump;
+  return RowsGap{jump, gap > 0 ? gap : 0};
+}
+// Keys in its own count that a tile of rows of so many tokens has at most.
+inline int rows_span(int window, int n_sink, long long tokens, int step, int max_len) {
+  const long long most = ((long long)n_sink + step - 1) / step * step + window + tokens - 1 + step;
+  return most < max_len ? (int)most : max_len;
+}
+
 __device__ __forceinline__ PagedSeq paged_seq_of(const PagedArgs& a, int s) {
   return paged_seq(a.len[s], a.row_start[s], a.row_start[s + 1], a.n_rows, a.max_new, a.max_len, a.table_pages, a.page_shift);
 }
@@ -64,9 +89,25 @@ struct PagedAppend {
 };
 bool launch_paged_append(const PagedArgs& a, const PagedAppend& src, int dtype, int d, hipStream_t s);
 
+struct PagedStore {
+  const void* q;  // nullptr: keys and values only
+  const void* k;
+  const void* v;
+  void* q_out;    // [n_rows][h_q][d]
+  const int32_t* pos;
+  long long q_token_stride, q_head_stride, token_stride, head_stride;  // bytes
+  long long pos_token_stride, pos_head_stride;
+  const int32_t* axes;  // rotary positions; nullptr: nothing is turned
+  long long axis_stride;
+  float theta;
+  int s0, s1;  // frequencies of the first two axes
+};
+bool launch_paged_store(const PagedArgs& a, const PagedStore& src, int dtype, int d, hipStream_t s);
+
 struct PagedPlan {
   int tile_rows, tiles;    // stacked rows per workgroup, tiles of max_new tokens
   int chunks, chunk_keys;  // tile kernel: key chunks of a sequence
+  int span;                // keys that a row tile looks at, at most
   int shares;              // few rows: workgroups of a KV head among which all entries are dealt, 0: one per tile
   long long workgroups;
   size_t scratch_bytes;

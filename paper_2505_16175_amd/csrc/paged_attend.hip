@@ -32,6 +32,7 @@ struct PagedOut {
   int tiles, chunks, chunk_keys;
   int shares;      // workgroups of a KV head among which the batch's blocks are dealt; 0: one for each unit, or the tile kernel
   int tile_rows;
+  int span;        // keys in their row tile's own count that a sequence has at most, see RowsGap
   int2* info;      // [units]: first share of a unit and the shares that have blocks of it
 };
 
@@ -42,7 +43,7 @@ struct PagedOut {
 template <typename E, int D>
 constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 
-// Where the workgroups' results meet.
+// Where the workgroups' results meet. pages: page numbers; WIN: of every 16 keys, in the row tile's own count.
 template <int D, int ROWS>
 struct RowsLds {
   int pages[PR_LIST];
@@ -51,31 +52,43 @@ struct RowsLds {
 };
 
 // Keys [k_begin, k_end) of one unit, a row tile of sequence s; slot: where its partial result goes, -1: it is the whole, and the output.
-template <typename E, int D, int RT>
+// WIN: keys in the unit's own count.
+template <typename E, int D, int RT, bool WIN>
 __device__ __forceinline__ void rows_unit(const PagedArgs& a, const PagedOut& o, RowsLds<D, 16 * RT>& lds, const PagedSeq& q, int s, int h,
-                                          int row0, int n_rows, int k_begin, int k_end, long long slot) {
+                                          int row0, int n_rows, int k_begin, int k_end, const RowsGap& gap, long long slot) {
   using L = RowsLayout<E, D>;
   using Block = RowsBlock<E, D>;
   constexpr int NE = L::NE, ROWS = 16 * RT;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r_heads = a.h_q / a.h_kv;
-  RowsWave<E, D, RT> rows;
+  RowsWave<E, D, RT, WIN> rows;
   rows.init(a, q, o.q, h, row0, n_rows);
   const float c2 = a.scale_log2;
   int seg = k_begin;  // first entry of the segment whose pages are listed
 
+  const int entry_end = WIN ? gap.entry(k_end - 1) + 1 : k_end;
   auto load = [&](Block& b, int key0) {
-    rows.load(b, a, h, key0, k_end,
-              [&](int key) { return __builtin_amdgcn_readfirstlane(lds.pages[(key >> a.page_shift) - (seg >> a.page_shift)]); });
+    if constexpr (WIN) {
+      const int entry0 = gap.entry(key0);
+      rows.load(b, a, h, entry0, entry_end,
+                [&](int entry) { return __builtin_amdgcn_readfirstlane(lds.pages[(key0 - seg + entry - entry0) >> 4]); });
+    } else {
+      rows.load(b, a, h, key0, k_end,
+                [&](int key) { return __builtin_amdgcn_readfirstlane(lds.pages[(key >> a.page_shift) - (seg >> a.page_shift)]); });
+    }
   };
-  auto compute = [&](Block& b, int key0) { rows.compute(b, key0, k_end, c2); };
+  auto compute = [&](Block& b, int key0) {
+    if constexpr (WIN) rows.compute(b, gap.entry(key0), entry_end, c2, a.window, a.n_sink);
+    else rows.compute(b, key0, k_end, c2);
+  };
 
   for (; seg < k_end; seg += PR_SEGMENT) {
     const int seg_end = min(k_end, k_end - seg > PR_SEGMENT ? seg + PR_SEGMENT : k_end);
-    const int first = seg >> a.page_shift, count = ((seg_end - 1) >> a.page_shift) - first + 1;
+    const int first = seg >> a.page_shift, count = WIN ? (seg_end - seg + 15) >> 4 : ((seg_end - 1) >> a.page_shift) - first + 1;
     __syncthreads();  // the last segment's list has been read
-    for (int i = tid; i < count; i += PR_NW * 64) lds.pages[i] = a.table[(size_t)s * a.table_pages + first + i];
+    for (int i = tid; i < count; i += PR_NW * 64)
+      lds.pages[i] = a.table[(size_t)s * a.table_pages + (WIN ? gap.entry(seg + 16 * i) >> a.page_shift : first + i)];
     __syncthreads();
     Block b0, b1;
     int key = seg + wave * L::BK;
@@ -89,6 +102,20 @@ __device__ __forceinline__ void rows_unit(const PagedArgs& a, const PagedOut& o,
       if (key + STEP < seg_end) load(b0, key + STEP);
       compute(b1, key);
       key += STEP;
+    }
+  }
+
+  if constexpr (L::QB == 2 && !L::F8) {  // E4M3 has no infinities
+    if (rows.any_not_finite()) {
+      rows.reset();
+      for (int key = k_begin + wave * L::BK; key < k_end; key += PR_NW * L::BK) {
+        Block b;
+        const int entry0 = WIN ? gap.entry(key) : key;
+        rows.load(b, a, h, entry0, entry_end, [&](int entry) {
+          return __builtin_amdgcn_readfirstlane(a.table[(size_t)s * a.table_pages + (entry >> a.page_shift)]);
+        });
+        rows.template compute<true>(b, entry0, entry_end, c2, a.window, a.n_sink);
+      }
     }
   }
 
@@ -149,18 +176,20 @@ __device__ __forceinline__ void rows_unit(const PagedArgs& a, const PagedOut& o,
 
 // A unit is a row tile of a sequence that has rows; its blocks are the PR_NW wavefronts' keys up to the last that a row sees.
 constexpr int PR_UNITS = 2048;  // units whose blocks a workgroup adds up
-template <int RT>
+template <int RT, bool WIN>
 __device__ __forceinline__ int unit_blocks(const PagedArgs& a, const PagedSeq& q, int tile, int step) {
   const int r_heads = a.h_q / a.h_kv;
   const long long all_rows = (long long)q.n * r_heads, row0 = (long long)tile * (16 * RT);
   if (row0 >= all_rows) return 0;
   const int last = (int)((min(row0 + 16 * RT, all_rows) - 1) / r_heads);
-  return max(1, (min(q.len, q.base + last + 1) + step - 1) / step);  // one at least: a unit that sees nothing has results too
+  int keys = min(q.len, q.base + last + 1);
+  if constexpr (WIN) keys -= rows_gap(a.window, a.n_sink, q.base + (int)(row0 / r_heads), step / PR_NW).gap;
+  return max(1, (keys + step - 1) / step);  // one at least: a unit that sees nothing has results too
 }
 
-template <typename E, int D, int RT>
+template <typename E, int D, int RT, bool WIN>
 __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_kernel(PagedArgs a, PagedOut o) {
-  constexpr int ROWS = 16 * RT, STEP = PR_NW * RowsLayout<E, D>::BK;
+  constexpr int ROWS = 16 * RT, BK = RowsLayout<E, D>::BK, STEP = PR_NW * BK;
   __shared__ RowsLds<D, ROWS> lds;
   const int tid = threadIdx.x;
   const int r_heads = a.h_q / a.h_kv;
@@ -187,7 +216,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     int n = 0;
     if (lane < units) {
       const PagedSeq q = paged_seq_of(a, lane / o.tiles);
-      n = unit_blocks<RT>(a, q, lane % o.tiles, STEP);
+      n = unit_blocks<RT, WIN>(a, q, lane % o.tiles, STEP);
       seqs[lane] = q;
     }
     const int sum = scan(n);
@@ -195,11 +224,11 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     if (lane == units - 1) before[units] = sum;
     all = __builtin_amdgcn_readlane(sum, units - 1);
   } else if (shared && units == 1) {  // one answer: nothing to add up
-    all = unit_blocks<RT>(a, paged_seq_of(a, 0), 0, STEP);
+    all = unit_blocks<RT, WIN>(a, paged_seq_of(a, 0), 0, STEP);
   } else if (shared) {
     for (int u0 = 0; u0 < units; u0 += PR_NW * 64) {
       const int v = u0 + tid;
-      const int n = v < units ? unit_blocks<RT>(a, paged_seq_of(a, v / o.tiles), v % o.tiles, STEP) : 0;
+      const int n = v < units ? unit_blocks<RT, WIN>(a, paged_seq_of(a, v / o.tiles), v % o.tiles, STEP) : 0;
       const int sum = scan(n);
       if (lane == 63) wave_sum[wave] = sum;
       __syncthreads();
@@ -249,15 +278,16 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     const int n_rows = (int)min((long long)q.n * r_heads - row0, (long long)ROWS);
     if (n_rows <= 0) return;  // not shared: a tile without rows
     const int stop = min(to, end);
-    const int k_end = min(stop == to ? 0x7fffffff : (stop - from) * STEP, min(q.len, q.base + (row0 + n_rows - 1) / r_heads + 1));
+    const RowsGap gap = WIN ? rows_gap(a.window, a.n_sink, q.base + row0 / r_heads, BK) : RowsGap{0, 0};
+    const int k_end = min(stop == to ? 0x7fffffff : (stop - from) * STEP, min(q.len, q.base + (row0 + n_rows - 1) / r_heads + 1) - gap.gap);
     const bool whole = at == from && stop == to;
     if (shared && h == 0 && at == from && tid == 0) {
       const int first = share_of(from);
       o.info[u] = make_int2(first, share_of(to - 1) - first + 1);
     }
     __syncthreads();  // the last unit's results have been read
-    rows_unit<E, D, RT>(a, o, lds, q, s, h, row0, n_rows, (at - from) * STEP, k_end,
-                        whole ? -1ll : (long long)h * (o.shares + units) + share + u);
+    rows_unit<E, D, RT, WIN>(a, o, lds, q, s, h, row0, n_rows, (at - from) * STEP, k_end, gap,
+                             whole ? -1ll : (long long)h * (o.shares + units) + share + u);
     at = stop;
   }
 }
@@ -279,7 +309,7 @@ __global__ __launch_bounds__((W == 1 ? PM_WAVES : W) * 64) void paged_merge_kern
   const int i = (int)(item / a.h_q), qh = (int)(item - (long long)i * a.h_q);
   if (i >= q.n) return;  // with W > 1: the whole workgroup
   const size_t at = (size_t)(q.row0 + i) * a.h_q + qh;
-  int n = q.len == 0 ? 1 : (q.len - 1) / o.chunk_keys + 1;  // chunks that answered
+  int n = q.len == 0 ? 1 : (min(q.len, o.span) - 1) / o.chunk_keys + 1;  // chunks that answered
   size_t first = at, stride = (size_t)a.n_rows * a.h_q;     // their rows among the partial results
   if (o.shares > 0) {
     const int r_heads = a.h_q / a.h_kv, h = qh / r_heads;
@@ -374,12 +404,19 @@ constexpr long long PT_FROM_ROWS = 32, PT_MOST_ROWS = 1 << 26;
 
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes) {
   PagedPlan p{};
-  const long long rows = (long long)a.max_new * (a.h_q / a.h_kv);
+  const int r_heads = a.h_q / a.h_kv;
+  const long long rows = (long long)a.max_new * r_heads;
   const bool tiled = dtype == QP_BF16 && d == 128 && rows > PT_FROM_ROWS && rows <= PT_MOST_ROWS;
   p.tile_rows = tiled ? PT_ROWS : rows <= 16 ? 16 : 32;
   p.tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
   p.chunks = 1;
-  p.chunk_keys = a.max_len;
+  // What a row tile has to look at: all entries, or the first ones and the windows of its tokens, each in whole blocks of keys
+  int max_len = a.max_len;
+  if (a.window > 0) {
+    const int tokens = std::min(a.max_new, (p.tile_rows + r_heads - 2) / r_heads + 1);
+    max_len = rows_span(a.window, a.n_sink, tokens, tiled ? 64 : dtype == QP_F32 ? 16 : 32, max_len);
+  }
+  p.span = p.chunk_keys = max_len;
   scratch_bytes = std::min(scratch_bytes, PAGED_ATTEND_SCRATCH);
   const long long units = (long long)a.n_seqs * p.tiles, cus = device_cu_count();
   if (!tiled) {
@@ -388,13 +425,13 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
     // four tokens of 16 sequences of the 72B heads over 8-bit pages of up to 32,768 entries 163 / 251, 180, 187; one token of 32
     // sequences of the 7B heads over up to 9,840 79.0 / 84.8, 89.8, 93.2, of one over 46,125 26.0 / 25.0, 27.6, 30.1.
     const int step = PR_NW * (dtype == QP_F32 ? 16 : 32);
-    const long long blocks = units * (((long long)a.max_len + step - 1) / step);
+    const long long blocks = units * (((long long)max_len + step - 1) / step);
     p.workgroups = units * a.h_kv;
     long long shares = std::min(std::max<long long>(1, (a.fp8 ? 2 : 1) * cus / a.h_kv), blocks);
     // Of a few blocks a workgroup per unit makes no second launch. us with shares / without, one token: f32 heads of 64 over 128
     // entries 8.7 / 7.6, 256 11.4 / 8.7, 333 11.2 / 10.8, 600 12.0 / 14.6, 1,200 11.2 / 23.9; 7B heads over 256 8.4 / 8.4 (one launch
     // both), 333 14.0 / 12.7, 600 14.4 / 15.9, 1,200 15.4 / 22.4, over 8-bit pools 333 13.8 / 11.5, 600 13.9 / 14.2, 1,200 15.8 / 20.2.
-    if (units > PR_UNITS || blocks > 0x7fffffff || a.max_len <= 2 * step) return p;
+    if (units > PR_UNITS || blocks > 0x7fffffff || max_len <= 2 * step) return p;
     const size_t per_share = (size_t)a.h_kv * p.tile_rows * (d + 1) * sizeof(float), info = (size_t)units * sizeof(int2);
     shares = std::min(shares, scratch_bytes < info ? 0ll : (long long)((scratch_bytes - info) / per_share) - units);
     if (shares < 2) return p;
@@ -406,26 +443,32 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   // One workgroup per compute unit at a time: four rounds of them, of at least 16 tiles of keys (four questions of up to 300
   // tokens over up to 46,125 entries: one round 544 us, two 580, three 555, four 506, six 531).
   const long long want = std::max<long long>(1, (4 * cus + units * a.h_kv - 1) / (units * a.h_kv));
-  long long keys = std::max<long long>(((a.max_len + want - 1) / want + 63) / 64 * 64, 16 * 64);
+  long long keys = std::max<long long>(((max_len + want - 1) / want + 63) / 64 * 64, 16 * 64);
   const size_t per_chunk = (size_t)a.n_rows * a.h_q * (d + 1) * sizeof(float);
-  long long chunks = (a.max_len + keys - 1) / keys;
+  long long chunks = (max_len + keys - 1) / keys;
   const long long fit = (long long)(scratch_bytes / per_chunk);
   if (chunks > fit) {
     chunks = fit >= 2 ? fit : 1;
-    keys = ((a.max_len + chunks - 1) / chunks + 63) / 64 * 64;
-    chunks = (a.max_len + keys - 1) / keys;
+    keys = ((max_len + chunks - 1) / chunks + 63) / 64 * 64;
+    chunks = (max_len + keys - 1) / keys;
   }
   if (chunks > 1) p.chunks = (int)chunks, p.chunk_keys = (int)keys, p.scratch_bytes = per_chunk * p.chunks;
   p.workgroups = paged_tile_blocks(a, p);
   return p;
 }
 
+template <typename E, int D, bool WIN>
+static void launch_rows(const PagedArgs& a, const PagedOut& o, const PagedPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)p.workgroups), block(PR_NW * 64);
+  if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1, WIN>), grid, block, 0, s, a, o);
+  else hipLaunchKernelGGL((paged_rows_kernel<E, D, 2, WIN>), grid, block, 0, s, a, o);
+}
+
 template <typename E, typename T, int D>
 static bool attend_as(const PagedArgs& a, const PagedOut& o, const PagedPlan& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.workgroups), block(PR_NW * 64);
   if (p.tile_rows == PT_ROWS) launch_paged_tiles(a, p, o.q, o.out, o.lse, o.part_o, o.part_lse, s);
-  else if (p.tile_rows == 16) hipLaunchKernelGGL((paged_rows_kernel<E, D, 1>), grid, block, 0, s, a, o);
-  else hipLaunchKernelGGL((paged_rows_kernel<E, D, 2>), grid, block, 0, s, a, o);
+  else if (a.window > 0) launch_rows<E, D, true>(a, o, p, s);
+  else launch_rows<E, D, false>(a, o, p, s);
   if (p.chunks > 1 || p.shares > 0) {
     const dim3 merge((unsigned)merge_blocks(a, p));
     if (merge_rows(a, p) == 1) hipLaunchKernelGGL((paged_merge_kernel<T, D, PM_SHARE>), merge, dim3(PM_SHARE * 64), 0, s, a, o);
@@ -442,12 +485,13 @@ bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, vo
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;
-  o.shares = p.shares, o.tile_rows = p.tile_rows;
+  o.shares = p.shares, o.tile_rows = p.tile_rows, o.span = p.span;
   const size_t part_rows = p.shares > 0 ? (size_t)(p.shares + a.n_seqs * p.tiles) * a.h_kv * p.tile_rows : (size_t)p.chunks * a.n_rows * a.h_q;
   o.part_o = (float*)scratch;
   o.part_lse = o.part_o + part_rows * d;
   o.info = (int2*)(o.part_lse + part_rows);  // part_rows is even
   if (dtype == QP_F32) return d == 64 ? attend_as<float, float, 64>(a, o, p, s) : attend_as<float, float, 128>(a, o, p, s);
+  if (a.fp8 == QP_CACHE_FP8_E4M3_SCALED) return attend_as<ScaledCode, bf16_t, 128>(a, o, p, s);
   if (a.fp8) return attend_as<uint8_t, bf16_t, 128>(a, o, p, s);
   return d == 64 ? attend_as<bf16_t, bf16_t, 64>(a, o, p, s) : attend_as<bf16_t, bf16_t, 128>(a, o, p, s);
 }

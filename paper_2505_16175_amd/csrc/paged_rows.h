@@ -14,19 +14,21 @@
 #pragma once
 #include "paged.h"
 
+#include <type_traits>
+
 namespace qp {
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pr_bf16x8;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float pr_f32x4;
 typedef unsigned int pr_u32x4 __attribute__((ext_vector_type(4)));
 
-// 8 E4M3 bytes -> 8 bf16 (exact)
-__device__ __forceinline__ pr_u32x4 pr_widen8(unsigned lo, unsigned hi) {
+// 8 E4M3 bytes, times a power of two, -> 8 bf16 (exact)
+__device__ __forceinline__ pr_u32x4 pr_widen8(unsigned lo, unsigned hi, float scale = 1.f) {
   pr_u32x4 o;
-  o.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
-  o.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
-  o.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
-  o.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+  o.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  o.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  o.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  o.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   return o;
 }
 
@@ -52,10 +54,14 @@ __device__ __forceinline__ void pr_join(float& sum, float plus, float minus) {
   if (minus > 0.f) sum += -INFINITY;
 }
 
-// E: the pool's element: float, bf16_t or uint8_t (E4M3, with bf16 rows).
+// E: the pool's element: float, bf16_t, uint8_t (E4M3, with bf16 rows) or ScaledCode (the same with scales). A tile of 16 keys is one
+// block of those, so its scales are two numbers, which the widening takes along.
+struct ScaledCode {
+  uint8_t code;
+};
 template <typename E, int D>
 struct RowsLayout {
-  static constexpr bool F32 = sizeof(E) == 4, F8 = sizeof(E) == 1;
+  static constexpr bool F32 = sizeof(E) == 4, F8 = sizeof(E) == 1, SCALED = std::is_same_v<E, ScaledCode>;
   static constexpr int TILES = F32 ? 1 : 2;          // tiles of 16 keys in a block
   static constexpr int BK = 16 * TILES;              // keys per block
   static constexpr int NE = D / 16;                  // elements of a V row per lane, and products of one V block
@@ -87,7 +93,7 @@ __device__ __forceinline__ void rows_load_k(const unsigned char* base, int l16, 
 // Products of 16 keys (k) with 16 rows (q); KEYS_ARE_ROWS: result rows are keys and columns query rows (else the other way).
 template <typename E, int D, bool KEYS_ARE_ROWS>
 __device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout<E, D>::KL],
-                                                  const pr_u32x4 (&q)[RowsLayout<E, D>::QF]) {
+                                                  const pr_u32x4 (&q)[RowsLayout<E, D>::QF], float scale = 1.f) {
   using L = RowsLayout<E, D>;
   pr_f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if constexpr (L::F32) {
@@ -103,7 +109,7 @@ __device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout
 #pragma unroll
     for (int st = 0; st < L::QF; ++st) {
       pr_u32x4 raw;
-      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1]);
+      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1], scale);
       else raw = k[st];
       const pr_bf16x8 x = __builtin_bit_cast(pr_bf16x8, raw), y = __builtin_bit_cast(pr_bf16x8, q[st]);
       s = KEYS_ARE_ROWS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, s, 0, 0, 0)
@@ -124,11 +130,12 @@ struct RowsBlock {
   using L = RowsLayout<E, D>;
   pr_u32x4 k[L::TILES][L::KL];
   unsigned v[L::VK][L::VW];
+  float ks[L::SCALED ? L::TILES : 1], vs[L::SCALED ? L::TILES : 1];  // the tiles' scales
   int ok;  // bit t: tile t's page is there
 };
 
-// Online softmax of a wavefront's RT tiles of 16 stacked rows over blocks of keys.
-template <typename E, int D, int RT>
+// Online softmax of a wavefront's RT tiles of 16 stacked rows over blocks of keys. WIN: rows see a window and the first entries.
+template <typename E, int D, int RT, bool WIN = false>
 struct RowsWave {
   using L = RowsLayout<E, D>;
   using Block = RowsBlock<E, D>;
@@ -138,7 +145,28 @@ struct RowsWave {
   float m[RT], l[RT];    // reference (log2 units), and this lane's part of the denominator
   int lim[RT];           // last entry that this lane's row sees
   int lim_min;           // and the tile's first row
+  int lim_max;           // and its last, WIN only
   int l16, g;
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m[t] = PR_NONE;
+      l[t] = 0.f;
+#pragma unroll
+      for (int e = 0; e < NE; ++e) acc[t][e] = pr_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ bool any_not_finite() const {
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < NE; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bad = bad || pr_not_finite(acc[t][e][r]);
+    return __any(bad);
+  }
 
   // rows row0 .. row0 + n_rows - 1 (at most 16 RT) of the sequence's stacked rows of head h
   __device__ __forceinline__ void init(const PagedArgs& a, const PagedSeq& q, const void* queries, int h, int row0, int n_rows) {
@@ -146,6 +174,7 @@ struct RowsWave {
     l16 = lane & 15;
     g = lane >> 4;
     lim_min = q.base + row0 / r_heads;
+    if constexpr (WIN) lim_max = q.base + (row0 + n_rows - 1) / r_heads;
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const int row = row0 + min(16 * t + l16, n_rows - 1), i = row / r_heads;
@@ -154,11 +183,8 @@ struct RowsWave {
                                ((size_t)(q.row0 + i) * a.h_q + (size_t)h * r_heads + (row - i * r_heads)) * (D * L::QB);
 #pragma unroll
       for (int u = 0; u < L::QF; ++u) qf[t][u] = *(const pr_u32x4*)(p + rows_q_byte<E, D>(u, g));
-      m[t] = PR_NONE;
-      l[t] = 0.f;
-#pragma unroll
-      for (int e = 0; e < NE; ++e) acc[t][e] = pr_f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    reset();
   }
 
   // Requests the block of keys from key0 on; page_of(key): the page number of the table, the same in all lanes.
@@ -172,7 +198,11 @@ struct RowsWave {
       const int page = page_of(key < k_end ? key : key0);
       const bool ok = paged_page_ok(page, a.n_pages);
       b.ok |= ok && key < k_end ? 1 << t : 0;
-      const size_t at = paged_row(ok ? page : 0, h, key & ((1 << a.page_shift) - 1), a.h_kv, a.page_shift) * L::ROWB;
+      const size_t row = paged_row(ok ? page : 0, h, key & ((1 << a.page_shift) - 1), a.h_kv, a.page_shift), at = row * L::ROWB;
+      if constexpr (L::SCALED) {
+        b.ks[t] = a.k_scale[row >> 4];
+        b.vs[t] = a.v_scale[row >> 4];
+      }
       rows_load_k<E, D>((const unsigned char*)a.k + at, l16, g, b.k[t]);
       const unsigned char* vb = (const unsigned char*)a.v + at;
 #pragma unroll
@@ -193,9 +223,13 @@ struct RowsWave {
     }
   }
 
-  __device__ __forceinline__ void compute(Block& b, int key0, int k_end, float c2) {
+  // CAREFUL: values that are not finite are looked for in blocks that every row sees whole, too: the second bf16 term of a numerator may be 0 or
+  // negative, and times an infinity that makes NaN of it.
+  template <bool CAREFUL = false>
+  __device__ __forceinline__ void compute(Block& b, int key0, int k_end, float c2, int window = 0, int n_sink = 0) {
     if (b.ok == 0) return;
-    const bool whole = b.ok == (1 << L::TILES) - 1 && key0 + L::BK <= k_end && key0 + L::BK - 1 <= lim_min;
+    bool whole = !CAREFUL && b.ok == (1 << L::TILES) - 1 && key0 + L::BK <= k_end && key0 + L::BK - 1 <= lim_min;
+    if constexpr (WIN) whole = whole && (key0 > lim_max - window || key0 + L::BK <= n_sink);
     if (!whole) {
       // V of entries that are not there may hold anything: 0 times it is not 0
 #pragma unroll
@@ -210,10 +244,12 @@ struct RowsWave {
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
       for (int y = 0; y < L::TILES; ++y) {
-        const pr_f32x4 st = rows_products<E, D, true>(b.k[y], qf[t]);
+        const pr_f32x4 st = rows_products<E, D, true>(b.k[y], qf[t], L::SCALED ? b.ks[y] : 1.f);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool seen = whole || (((b.ok >> y) & 1) && key0 + 16 * y + 4 * g + r <= min(lim[t], k_end - 1));
+          const int key = key0 + 16 * y + 4 * g + r;
+          bool seen = whole || (((b.ok >> y) & 1) && key <= min(lim[t], k_end - 1));
+          if constexpr (WIN) seen = seen && (whole || key > lim[t] - window || key < n_sink);
           p[t][4 * y + r] = seen ? st[r] : -INFINITY;
         }
       }
@@ -286,8 +322,9 @@ struct RowsWave {
           lo[t][j] = (__bf16)(p[t][j] - (float)hi[t][j]);
         }
       auto pair = [&](int j, int y) {  // elements 2 y and 2 y + 1 of key j, as bf16
-        if constexpr (L::F8) return (unsigned)__builtin_bit_cast(unsigned, (y & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], 1.f, true)
-                                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], 1.f, false));
+        const float scale = L::SCALED ? b.vs[j >> 2] : 1.f;
+        if constexpr (L::F8) return (unsigned)__builtin_bit_cast(unsigned, (y & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, true)
+                                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, false));
         else return b.v[j][y];
       };
       bool bad = false;

@@ -113,7 +113,8 @@ qp_status qp_paged_append_rope(const qp_layout* layout, const qp_paged_cache* ca
  * sees no entry (the sequence has fewer than its new rows, or none of its pages is there) gets zeros and -infinity. Arithmetic as qp_group_attend: f32
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (to two bf16 terms in calls of up to
  * 32 stacked rows, max_new * H_q / H_kv, and over heads of 64), never in the sums behind lse. All rows of a call take the same way, so
- * a row's last bits depend on max_new. What a row does not see does not reach its result, infinities and NaN included. Logits scale * q.k of
+ * a row's last bits depend on max_new. What a row does not see does not reach its result, infinities and NaN included; an
+ * infinite value that it sees makes its element infinite, or NaN. Logits scale * q.k of
  * up to 2^28 in size are computed; those below -2^29 weigh nothing, as -infinity does, and a row that sees nothing else is one that sees
  * no entry; of a row with one above 2^28 nothing is promised.
  *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups

@@ -211,6 +211,7 @@ __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const Paged
       RowsWave<E, MF_D, 1, WINDOW> rows;
       const int count = min(16, n_rows - row0 - half);
       rows.init(a.pg, seq, a.q, h, row0 + half, count);
+      rows.be_careful();
       const int entries = min(seq.len, seq.base + (row0 + half + count - 1) / r_heads + 1);
       const int end = min(key_end, WINDOW ? entries - gap.gap : entries);
       for (int key = key_begin; key < end; key += RowsLayout<E, MF_D>::BK) {
@@ -219,7 +220,7 @@ __device__ __forceinline__ void paged_finish(const PagedTileArgs& a, const Paged
         rows.load(b, a.pg, h, at, at_end, [&](int k) {
           return __builtin_amdgcn_readfirstlane(a.pg.table[(size_t)seq_no * a.pg.table_pages + (k >> a.pg.page_shift)]);
         });
-        rows.template compute<true>(b, at, at_end, a.scale_log2, a.pg.window, a.pg.n_sink);
+        rows.compute(b, at, at_end, a.scale_log2, a.pg.window, a.pg.n_sink);
       }
       const float den = rows.denominator(0);
       const bool none = den == 0.f;

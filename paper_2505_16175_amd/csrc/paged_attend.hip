@@ -105,20 +105,6 @@ __device__ __forceinline__ void rows_unit(const PagedArgs& a, const PagedOut& o,
     }
   }
 
-  if constexpr (L::QB == 2 && !L::F8) {  // E4M3 has no infinities
-    if (rows.any_not_finite()) {
-      rows.reset();
-      for (int key = k_begin + wave * L::BK; key < k_end; key += PR_NW * L::BK) {
-        Block b;
-        const int entry0 = WIN ? gap.entry(key) : key;
-        rows.load(b, a, h, entry0, entry_end, [&](int entry) {
-          return __builtin_amdgcn_readfirstlane(a.table[(size_t)s * a.table_pages + (entry >> a.page_shift)]);
-        });
-        rows.template compute<true>(b, entry0, entry_end, c2, a.window, a.n_sink);
-      }
-    }
-  }
-
   // the wavefronts' results meet in LDS
 #pragma unroll
   for (int t = 0; t < RT; ++t) {

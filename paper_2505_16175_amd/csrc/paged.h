@@ -107,6 +107,7 @@ bool launch_paged_store(const PagedArgs& a, const PagedStore& src, int dtype, in
 struct PagedPlan {
   int tile_rows, tiles;    // stacked rows per workgroup, tiles of max_new tokens
   int chunks, chunk_keys;  // tile kernel: key chunks of a sequence
+  int per_unit;            // few rows of a window: workgroups of a KV head for each row tile of a sequence
   int span;                // keys that a row tile looks at, at most
   int shares;              // few rows: workgroups of a KV head among which all entries are dealt, 0: one per tile
   long long workgroups;

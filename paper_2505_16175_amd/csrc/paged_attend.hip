@@ -16,6 +16,7 @@
 #include "paged_rows.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace qp {
 
@@ -31,6 +32,7 @@ struct PagedOut {
   float* part_lse; // the same without d, log2 units
   int tiles, chunks, chunk_keys;
   int shares;      // workgroups of a KV head among which the batch's blocks are dealt; 0: one for each unit, or the tile kernel
+  int per_unit;    // of a window: those of each unit, which share its blocks only
   int tile_rows;
   int span;        // keys in their row tile's own count that a sequence has at most, see RowsGap
   int2* info;      // [units]: first share of a unit and the shares that have blocks of it
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
   __shared__ PagedSeq seqs[64];
   const int lane = tid & 63, wave = tid >> 6;
   const int share = blockIdx.x / a.h_kv, units = a.n_seqs * o.tiles;
-  const bool few = shared && units <= 64 && units > 1;
+  const bool few = !WIN && shared && units <= 64 && units > 1;
   int begin = 0, end = 1, u = share, all = 0, per = 0, more = 0;
   auto scan = [&](int sum) {
 #pragma unroll
@@ -198,7 +200,19 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     }
     return sum;
   };
-  if (few) {
+  if constexpr (WIN) {
+    if (shared) {
+      u = share / o.per_unit;
+      all = unit_blocks<RT, WIN>(a, paged_seq_of(a, u / o.tiles), u % o.tiles, STEP);
+      const int parts = min(o.per_unit, all), part = share - u * o.per_unit;
+      if (part >= parts) return;
+      if (part == 0 && h == 0 && tid == 0) o.info[u] = make_int2(u * o.per_unit, parts);
+      per = all / parts;
+      more = all - per * parts;
+      begin = part * per + min(part, more);
+      end = begin + per + (part < more);
+    }
+  } else if (few) {
     int n = 0;
     if (lane < units) {
       const PagedSeq q = paged_seq_of(a, lane / o.tiles);
@@ -231,7 +245,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     __syncthreads();
     all = __builtin_amdgcn_readfirstlane(all);  // the same in all lanes, which the compiler cannot see, nor of what comes from LDS
   }
-  if (shared) {
+  if (!WIN && shared) {
     const int shares = min(o.shares, all);  // each has a block at least
     if (share >= shares) return;
     per = all / shares;
@@ -248,7 +262,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     return block < longer ? block / (per + 1) : more + (block - longer) / per;
   };
   for (int at = begin; at < end; ++u) {
-    const bool listed = shared && units > 1;
+    const bool listed = !WIN && shared && units > 1;
     const int from = listed ? __builtin_amdgcn_readfirstlane(before[u]) : 0, to = listed ? __builtin_amdgcn_readfirstlane(before[u + 1]) : shared ? all : 1;
     if (from == to) continue;
     const int s = u / o.tiles, row0 = (u - s * o.tiles) * ROWS;
@@ -267,7 +281,7 @@ __global__ __launch_bounds__(PR_NW * 64, (pr_waves<E, D>())) void paged_rows_ker
     const RowsGap gap = WIN ? rows_gap(a.window, a.n_sink, q.base + row0 / r_heads, BK) : RowsGap{0, 0};
     const int k_end = min(stop == to ? 0x7fffffff : (stop - from) * STEP, min(q.len, q.base + (row0 + n_rows - 1) / r_heads + 1) - gap.gap);
     const bool whole = at == from && stop == to;
-    if (shared && h == 0 && at == from && tid == 0) {
+    if (!WIN && shared && h == 0 && at == from && tid == 0) {
       const int first = share_of(from);
       o.info[u] = make_int2(first, share_of(to - 1) - first + 1);
     }
@@ -419,7 +433,20 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
     // both), 333 14.0 / 12.7, 600 14.4 / 15.9, 1,200 15.4 / 22.4, over 8-bit pools 333 13.8 / 11.5, 600 13.9 / 14.2, 1,200 15.8 / 20.2.
     if (units > PR_UNITS || blocks > 0x7fffffff || max_len <= 2 * step) return p;
     const size_t per_share = (size_t)a.h_kv * p.tile_rows * (d + 1) * sizeof(float), info = (size_t)units * sizeof(int2);
-    shares = std::min(shares, scratch_bytes < info ? 0ll : (long long)((scratch_bytes - info) / per_share) - units);
+    const long long fit = scratch_bytes < info ? 0ll : (long long)((scratch_bytes - info) / per_share) - units;
+    if (a.window > 0) {
+      // Windows are alike in length, so each unit has as many workgroups as the others: none has parts of two units, which costs it
+      // the start and the end of both, and none adds up the others' blocks. As many as end first, in blocks of keys, with three for start and end.
+      const long long n = (max_len + step - 1) / step, slots = shares;
+      double least = 0;
+      for (long long c = 1; c <= n && c * units <= std::min(4 * slots + units, PR_UNITS * 64ll); ++c) {
+        const double cost = (double)((c * units + slots - 1) / slots) * ((n + c - 1) / c + 3) + (c > 1 ? 3 : 0);
+        if (c * units <= std::max(fit, units) && (p.per_unit == 0 || cost < least)) p.per_unit = (int)c, least = cost;
+      }
+      if (p.per_unit <= 1) return p;
+      shares = p.per_unit * units;
+    }
+    shares = std::min(shares, fit);
     if (shares < 2) return p;
     p.shares = (int)shares;
     p.workgroups = shares * a.h_kv;
@@ -431,6 +458,23 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   const long long want = std::max<long long>(1, (4 * cus + units * a.h_kv - 1) / (units * a.h_kv));
   long long keys = std::max<long long>(((max_len + want - 1) / want + 63) / 64 * 64, 16 * 64);
   const size_t per_chunk = (size_t)a.n_rows * a.h_q * (d + 1) * sizeof(float);
+  if (a.window > 0) {
+    // Windows are alike in length, so a launch ends in rounds of workgroups, one per compute unit at a time, on each XCD's share of them
+    // (see the mapping of workgroups there): as many chunks as end first. In tiles of keys, with seven for a workgroup's start and end and what
+    // a second launch and the chunks' partial rows cost. us with 1 / 2 / 3 / 4 / 6 / 8 chunks of a window of 8,192 and 100 first entries, 7B heads: 300
+    // tokens 241 / 137 / 104 / 87 / 68 / 89, of four sequences 240 / 254 / 213 / 227 / 231 / 222, up to 300 of four 240 / 162 / 197 / 165 / 180 / 184, 20 of
+    // 16 226 / 131 / 99 / 84 / 105 / 95; up to 300 of four, window 4,096, 72B heads with scales 162 / 206 / 217 / 228 / 228 / 227.
+    const long long n = (max_len + 63) / 64;
+    const double blocks = std::min((double)p.tiles, std::ceil((double)a.n_rows * r_heads / PT_ROWS / a.n_seqs + 0.5));  // of rows, per sequence
+    const int xcds = 8 % a.h_kv == 0 ? 8 / a.h_kv : 1, heads = a.h_kv % 8 == 0 ? a.h_kv / 8 : 1;                // of a head, of an XCD
+    double least = 0;
+    for (long long c = 1; c <= std::min<long long>(n, 64); ++c) {
+      double wgs = (double)((a.n_seqs * c + xcds - 1) / xcds) * heads * blocks;  // on the XCD with most
+      if (8 % a.h_kv != 0 && a.h_kv % 8 != 0) wgs = (double)a.n_seqs * c * a.h_kv * blocks / 8;
+      const double cost = std::ceil(wgs * 8 / cus) * ((n + c - 1) / c + 7) + (c > 1 ? 3 + c * (double)per_chunk / 14e6 : 0);
+      if (c == 1 || cost < least) keys = (n + c - 1) / c * 64, least = cost;
+    }
+  }
   long long chunks = (max_len + keys - 1) / keys;
   const long long fit = (long long)(scratch_bytes / per_chunk);
   if (chunks > fit) {
@@ -471,7 +515,7 @@ bool launch_paged_attend(const PagedArgs& a, int dtype, int d, const void* q, vo
   PagedOut o{};
   o.q = q, o.out = out, o.lse = lse;
   o.tiles = p.tiles, o.chunks = p.chunks, o.chunk_keys = p.chunk_keys;
-  o.shares = p.shares, o.tile_rows = p.tile_rows, o.span = p.span;
+  o.shares = p.shares, o.tile_rows = p.tile_rows, o.span = p.span, o.per_unit = p.per_unit;
   const size_t part_rows = p.shares > 0 ? (size_t)(p.shares + a.n_seqs * p.tiles) * a.h_kv * p.tile_rows : (size_t)p.chunks * a.n_rows * a.h_q;
   o.part_o = (float*)scratch;
   o.part_lse = o.part_o + part_rows * d;

@@ -175,6 +175,7 @@ struct PagedTileKind<PagedTileArgsOf<S, W>> {
   static constexpr bool PAGED = true, SCALED = S, WINDOW = W;
 };
 __device__ unsigned char paged_zeros[8 * 256];  // eight rows of a missing page
+__device__ float paged_one = 1.f;               // and their scale
 
 // A wavefront's 32 rows of a chunk (or of the whole): partial results, or the output. Where a result is not finite, a value that
 // some of its rows do not see may have reached them (0 times infinity): such rows are done again, 16 at a time, by the arithmetic
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(MF_NT, 2) void attend_mfma_kernel(Args a) {
   if constexpr (SCALED) k_scales = a.pg.k_scale, v_scales = a.pg.v_scale;
   auto place = [&](Stream& s, const unsigned char* pool, const float* scales, const Eight& e, unsigned c0, unsigned c1) {
     if constexpr (PAGED) {
-      if constexpr (SCALED) s.scale = scales + e.at / (16 * CROW);
+      if constexpr (SCALED) s.scale = e.ok ? scales + e.at / (16 * CROW) : &paged_one;
       s.src = e.ok ? pool + e.at : (const unsigned char*)paged_zeros;
       const int sub = lane >> 4;  // keys past the last one repeat it: masked, never used
       s.o0 = (unsigned)min(sub, e.left) * CROW + (c0 >> (F8 ? 1 : 0));

@@ -119,6 +119,38 @@ __device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout
   return s;
 }
 
+// S^T of a block's tiles of keys with RT tiles of rows.
+template <typename E, int D, int RT, class Block>
+__device__ __forceinline__ void rows_scores(const Block& b, const pr_u32x4 (&q)[RT][RowsLayout<E, D>::QF],
+                                            pr_f32x4 (&s)[RT][RowsLayout<E, D>::TILES]) {
+  using L = RowsLayout<E, D>;
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int y = 0; y < L::TILES; ++y) s[t][y] = pr_f32x4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (L::F32) {
+#pragma unroll
+    for (int u = 0; u < L::KL; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          s[t][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.k[0][u][e]), __uint_as_float(q[t][u][e]), s[t][0], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int st = 0; st < L::QF; ++st)
+#pragma unroll
+      for (int y = 0; y < L::TILES; ++y) {
+        pr_u32x4 raw;
+        if constexpr (L::F8) raw = pr_widen8(b.k[y][st >> 1][2 * (st & 1)], b.k[y][st >> 1][2 * (st & 1) + 1], b.key_scale(y));
+        else raw = b.k[y][st];
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          s[t][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, raw), __builtin_bit_cast(pr_bf16x8, q[t][st]), s[t][y], 0, 0, 0);
+      }
+  }
+}
+
 // A row's reference (log2 units) before its first visible entry, and its lowest one. c s - m is one multiply-add, so with m rounded from
 // a product all numerators of a row carry the same factor, 2 to the power of what that rounding lost: it cancels as long as it is finite. A
 // block of nothing but huge negative logits would make it 2^(2^-24 |m|), an infinity that no later reference takes back.
@@ -130,8 +162,15 @@ struct RowsBlock {
   using L = RowsLayout<E, D>;
   pr_u32x4 k[L::TILES][L::KL];
   unsigned v[L::VK][L::VW];
-  float ks[L::SCALED ? L::TILES : 1], vs[L::SCALED ? L::TILES : 1];  // the tiles' scales
-  int ok;  // bit t: tile t's page is there
+  float scales;  // SCALED: lanes 0 and 1 (of every four) have those of the tiles' keys, 2 and 3 of their values
+  int ok;        // bit t: tile t's page is there
+  __device__ __forceinline__ float key_scale(int tile) const { return L::SCALED ? scale_of(tile, tile) : 1.f; }
+  __device__ __forceinline__ float value_scale(int tile) const { return L::SCALED ? scale_of(tile, 2 + tile) : 1.f; }
+  // Of a tile without entries any bits may be there, and 0 times a NaN is not 0.
+  __device__ __forceinline__ float scale_of(int tile, int lane) const {
+    const unsigned bits = (unsigned)__builtin_amdgcn_readlane(__float_as_uint(scales), lane);
+    return __uint_as_float((ok >> tile) & 1 ? bits : 0x3f800000u);
+  }
 };
 
 // Online softmax of a wavefront's RT tiles of 16 stacked rows over blocks of keys. WIN: rows see a window and the first entries.
@@ -174,6 +213,7 @@ struct RowsWave {
   template <class PageOf>
   __device__ __forceinline__ void load(Block& b, const PagedArgs& a, int h, int key0, int k_end, PageOf page_of) const {
     b.ok = 0;
+    size_t rows[L::TILES];
 #pragma unroll
     for (int t = 0; t < L::TILES; ++t) {
       const int key = key0 + 16 * t;
@@ -182,10 +222,7 @@ struct RowsWave {
       const bool ok = paged_page_ok(page, a.n_pages);
       b.ok |= ok && key < k_end ? 1 << t : 0;
       const size_t row = paged_row(ok ? page : 0, h, key & ((1 << a.page_shift) - 1), a.h_kv, a.page_shift), at = row * L::ROWB;
-      if constexpr (L::SCALED) {
-        b.ks[t] = a.k_scale[row >> 4];
-        b.vs[t] = a.v_scale[row >> 4];
-      }
+      rows[t] = row;
       rows_load_k<E, D>((const unsigned char*)a.k + at, l16, g, b.k[t]);
       const unsigned char* vb = (const unsigned char*)a.v + at;
 #pragma unroll
@@ -204,6 +241,24 @@ struct RowsWave {
         }
       }
     }
+    if constexpr (L::SCALED) {
+      // One load of them all, in order with the others: as scalar loads, which end in any order, a block's were waited for together with the
+      // next one's, just requested (four tokens of 16 sequences of the 72B heads over up to 32,768 entries 163 us).
+      const int lane = threadIdx.x & 63;
+      b.scales = ((lane & 2) ? a.v_scale : a.k_scale)[((lane & 1) ? rows[L::TILES - 1] : rows[0]) >> 4];
+    }
+  }
+
+  // Whether some value of the block is an infinity or NaN: an element of which the exponent (of E4M3: everything but the sign) is all ones, to
+  // which its least bit is added and makes the next.
+  __device__ __forceinline__ bool values_not_finite(const Block& b) const {
+    constexpr unsigned ONES = L::F32 ? 0x7f800000u : L::F8 ? 0x7f7f7f7fu : 0x7f807f80u, LEAST = L::F32 ? 0x00800000u : L::F8 ? 0x01010101u : 0x00800080u;
+    unsigned found = 0;
+#pragma unroll
+    for (int j = 0; j < L::VK; ++j)
+#pragma unroll
+      for (int w = 0; w < L::VW; ++w) found |= (b.v[j][w] & ONES) + LEAST;
+    return __any((found & (L::F32 ? 0x80000000u : L::F8 ? 0x80808080u : 0x80008000u)) != 0);
   }
 
   // Values that are not finite are looked for in blocks that every row sees whole, too: the second bf16 term of a numerator may be 0 or
@@ -224,20 +279,29 @@ struct RowsWave {
         for (int w = 0; w < L::VW; ++w) b.v[j][w] = there ? b.v[j][w] : 0u;
       }
     }
+    // The products' chains side by side, and masks behind a branch: an element's is six instructions, of few blocks.
     float p[RT][L::VK];
+    {
+      pr_f32x4 st[RT][L::TILES];
+      rows_scores<E, D, RT>(b, qf, st);
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int j = 0; j < L::VK; ++j) p[t][j] = st[t][j >> 2][j & 3];
+    }
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int j = 0; j < L::VK; ++j) {
+          const int key = key0 + 16 * (j >> 2) + 4 * g + (j & 3);
+          bool seen = ((b.ok >> (j >> 2)) & 1) && key <= min(lim[t], k_end - 1);
+          if constexpr (WIN) seen = seen && (key > lim[t] - window || key < n_sink);
+          p[t][j] = seen ? p[t][j] : -INFINITY;
+        }
+    }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-#pragma unroll
-      for (int y = 0; y < L::TILES; ++y) {
-        const pr_f32x4 st = rows_products<E, D, true>(b.k[y], qf[t], L::SCALED ? b.ks[y] : 1.f);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = key0 + 16 * y + 4 * g + r;
-          bool seen = whole || (((b.ok >> y) & 1) && key <= min(lim[t], k_end - 1));
-          if constexpr (WIN) seen = seen && (whole || key > lim[t] - window || key < n_sink);
-          p[t][4 * y + r] = seen ? st[r] : -INFINITY;
-        }
-      }
       float mx = p[t][0];
 #pragma unroll
       for (int j = 1; j < L::VK; ++j) mx = fmaxf(mx, p[t][j]);
@@ -261,14 +325,7 @@ struct RowsWave {
     }
     const pr_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     if constexpr (L::F32) {
-      bool bad = false;
-      if (!whole) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int e = 0; e < NE; ++e) bad = bad || pr_not_finite(__uint_as_float(b.v[r][e]));
-      }
-      if (__any(bad)) {
+      if (!whole && values_not_finite(b)) {
 #pragma unroll
         for (int e = 0; e < NE; ++e)
 #pragma unroll
@@ -307,32 +364,35 @@ struct RowsWave {
           lo[t][j] = (__bf16)(p[t][j] - (float)hi[t][j]);
         }
       auto pair = [&](int j, int y) {  // elements 2 y and 2 y + 1 of key j, as bf16
-        const float scale = L::SCALED ? b.vs[j >> 2] : 1.f;
+        const float scale = b.value_scale(j >> 2);
         if constexpr (L::F8) return (unsigned)__builtin_bit_cast(unsigned, (y & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, true)
                                                                                   : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, false));
         else return b.v[j][y];
       };
-      bool bad = false;
-      if (!whole) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int y = 0; y < NE / 2; ++y) {
-            const unsigned w = pair(j, y);
-            bad = bad || pr_not_finite(bf16lo_to_f32(w)) || pr_not_finite(bf16hi_to_f32(w));
-          }
-      }
-      const bool guard = __any(bad);
+      const bool guard = !whole && values_not_finite(b);
       unsigned w[8];
 #pragma unroll
       for (int e = 0; e < NE; ++e) {
-        if ((e & 1) == 0) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = pair(j, e >> 1);
-        }
         pr_u32x4 f;  // element e of the lane's 8 keys
+        if constexpr (L::F8) {  // bytes of two keys are put side by side and then widened, half as many moves as the other way
+          if ((e & 1) == 0) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(w[2 * y + 1], w[2 * y], (e & 1) ? 0x07060302u : 0x05040100u);
+            for (int y = 0; y < 4; ++y) w[y] = __builtin_amdgcn_perm(b.v[2 * y + 1][e >> 2], b.v[2 * y][e >> 2], (e & 2) ? 0x07030602u : 0x05010400u);
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const float scale = b.value_scale(y >> 1);
+            f[y] = (e & 1) ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[y], scale, true))
+                           : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[y], scale, false));
+          }
+        } else {
+          if ((e & 1) == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pair(j, e >> 1);
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(w[2 * y + 1], w[2 * y], (e & 1) ? 0x07060302u : 0x05040100u);
+        }
         if (guard) {
           pr_u32x4 finite, fp, fm;
 #pragma unroll

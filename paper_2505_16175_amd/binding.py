@@ -642,26 +642,6 @@ def paged_append(layout, cache: PagedCache, batch: PagedBatch, k, v, pos):
     _check(st, "qp_paged_append")
 
 
-def _row_strides(stride, shape):
-    """(token, head) strides of rows in one run; of one token or head any stride does."""
-    n, h, _ = shape
-    if n == 1 or h == 1:
-        return 0 if n == 1 else stride[0], 0 if h == 1 else stride[1], stride[2]
-    return stride
-
-
-def _kv_strides(k, v, pos, shape, here):
-    sk, sv = _row_strides(k.stride(), shape), _row_strides(v.stride(), shape)
-    if sk != sv or sk[2] != 1:
-        raise ValueError("k and v: expected the same strides and rows in one run")
-    if pos.dtype is not torch.int32 or pos.shape != shape[:1] and pos.shape != shape[:2]:
-        raise ValueError("pos: expected int32 [n_rows] or [n_rows][H_kv]")
-    if k.get_device() != here or v.get_device() != here or pos.get_device() != here:
-        raise ValueError("expected tensors of the current GPU")
-    sp = pos.stride()
-    return sk, (sp[0], sp[1] if len(sp) == 2 else 0)
-
-
 class PagedRope:
     """Rotary positions of a call's rows: axes int32 [3][n_rows] (temporal, height and width index) or [n_rows] (the same on all), and how
     many of the head_dim / 2 frequencies turn by each axis. The values may change between calls, and between replays of a captured one."""
@@ -673,7 +653,7 @@ class PagedRope:
             raise ValueError("axes: expected int32 [3][n_rows] or [n_rows]")
         if axes.get_device() < 0 or not axes.is_contiguous():
             raise ValueError("axes: expected a contiguous tensor on the GPU")
-        self.axes, self.n_rows, self.device_index = axes, axes.shape[-1], axes.get_device()
+        self.axes, self.n_rows, self.device_index, self.head_dim = axes, axes.shape[-1], axes.get_device(), layout.head_dim
         self.c = qp_paged_rope(axes.data_ptr(), axes.shape[1] if axes.dim() == 2 else 0, theta, (ctypes.c_int32 * 3)(*section))
         self.ref = ctypes.byref(self.c)
 
@@ -682,25 +662,47 @@ def paged_append_rope(layout, cache: PagedCache, batch: PagedBatch, k, v, pos, r
     """paged_append of keys that are not rotated yet: k (and q [n_rows][H_q][d] of any strides whose rows are runs, into q_out, dense) turned
     by their rows' angles on the way. k, v, pos as in paged_append, in the layout's dtype."""
     here = _same_gpu(layout, cache, batch)
-    n, d, dt = batch.n_rows, layout.head_dim, _layout_dtype(layout)
-    shape = (n, layout.n_kv_heads, d)
+    h_kv, d, code = cache.made_for
+    n, dt = batch.n_rows, torch.float32 if code == QP_F32 else torch.bfloat16
+    shape, sp = (n, h_kv, d), pos.shape
     if k.dtype is not dt or v.dtype is not dt or k.shape != shape or v.shape != shape:
         raise ValueError(f"k and v: expected {dt} {shape}, got {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}")
-    sk, sp = _kv_strides(k, v, pos, shape, here)
-    if rope.n_rows != n or rope.device_index != here:
-        raise ValueError("rope: expected positions of the batch's rows on the current GPU")
-    if (q is None) != (q_out is None):
-        raise ValueError("expected q and q_out, or neither")
-    sq, q_at, out_at = (0, 0, 1), None, None
-    if q is not None:
+    if pos.dtype is not torch.int32 or sp != shape[:1] and sp != shape[:2]:
+        raise ValueError("pos: expected int32 [n_rows] or [n_rows][H_kv]")
+    if k.get_device() != here or v.get_device() != here or pos.get_device() != here:
+        raise ValueError("expected tensors of the current GPU")
+    token, head, one = k.stride()
+    if v.stride() != (token, head, one):                 # of one row or head, any stride does
+        vt, vh, one_v = v.stride()
+        if one != one_v or token != vt and n > 1 or head != vh and h_kv > 1:
+            one = 0
+    if one != 1:
+        raise ValueError("k and v: expected the same strides and rows in one run")
+    if n == 1:
+        token = 0
+    if h_kv == 1:
+        head = 0
+    if rope.n_rows != n or rope.device_index != here or rope.head_dim != d:
+        raise ValueError("rope: expected positions of the batch's rows for this head_dim on the current GPU")
+    sp = pos.stride()
+    q_at = out_at = None
+    q_token = q_head = 0
+    if q is not None and q_out is not None:
         shape = (n, layout.n_q_heads, d)
         if q.dtype is not dt or q.shape != shape or q.get_device() != here:
             raise ValueError(f"q: expected {dt} {shape} on the current GPU, got {q.dtype} {tuple(q.shape)}")
-        sq, q_at, out_at = _row_strides(q.stride(), shape), q.data_ptr(), _dense(q_out, dt, shape, "q_out", here)
-        if sq[2] != 1:
+        q_token, q_head, one = q.stride()
+        if one != 1:
             raise ValueError("q: expected rows in one run")
-    st = lib().qp_paged_append_rope(ctypes.byref(layout), cache.ref, batch.of(cache), rope.ref, q_at, sq[0], sq[1], k.data_ptr(), v.data_ptr(),
-                                    sk[0], sk[1], pos.data_ptr(), sp[0], sp[1], out_at, _stream())
+        if n == 1:
+            q_token = 0
+        if shape[1] == 1:
+            q_head = 0
+        q_at, out_at = q.data_ptr(), _dense(q_out, dt, shape, "q_out", here)
+    elif q is not None or q_out is not None:
+        raise ValueError("expected q and q_out, or neither")
+    st = lib().qp_paged_append_rope(ctypes.byref(layout), cache.ref, batch.of(cache), rope.ref, q_at, q_token, q_head, k.data_ptr(), v.data_ptr(),
+                                    token, head, pos.data_ptr(), sp[0], sp[1] if len(sp) == 2 else 0, out_at, _stream())
     _check(st, "qp_paged_append_rope")
 
 

@@ -101,6 +101,7 @@ struct PagedStore {
   long long axis_stride;
   float theta;
   int s0, s1;  // frequencies of the first two axes
+  double low[8], high[8];  // filled by the launch
 };
 bool launch_paged_store(const PagedArgs& a, const PagedStore& src, int dtype, int d, hipStream_t s);
 

@@ -90,30 +90,23 @@ __device__ __forceinline__ void rows_load_k(const unsigned char* base, int l16, 
   for (int u = 0; u < RowsLayout<E, D>::KL; ++u) k[u] = *(const pr_u32x4*)(base + (at + rows_k_byte<E, D>(u, g)));
 }
 
-// Products of 16 keys (k) with 16 rows (q); KEYS_ARE_ROWS: result rows are keys and columns query rows (else the other way).
-template <typename E, int D, bool KEYS_ARE_ROWS>
-__device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout<E, D>::KL],
-                                                  const pr_u32x4 (&q)[RowsLayout<E, D>::QF], float scale = 1.f) {
+// Products of 16 keys (k) with 16 rows (q): result rows are query rows, columns keys.
+template <typename E, int D>
+__device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout<E, D>::KL], const pr_u32x4 (&q)[RowsLayout<E, D>::QF]) {
   using L = RowsLayout<E, D>;
   pr_f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if constexpr (L::F32) {
 #pragma unroll
     for (int u = 0; u < L::KL; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = __uint_as_float(k[u][e]), y = __uint_as_float(q[u][e]);
-        s = KEYS_ARE_ROWS ? __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, s, 0, 0, 0)
-                          : __builtin_amdgcn_mfma_f32_16x16x4f32(y, x, s, 0, 0, 0);
-      }
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[u][e]), __uint_as_float(k[u][e]), s, 0, 0, 0);
   } else {
 #pragma unroll
     for (int st = 0; st < L::QF; ++st) {
       pr_u32x4 raw;
-      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1], scale);
+      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1]);
       else raw = k[st];
-      const pr_bf16x8 x = __builtin_bit_cast(pr_bf16x8, raw), y = __builtin_bit_cast(pr_bf16x8, q[st]);
-      s = KEYS_ARE_ROWS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, s, 0, 0, 0)
-                        : __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, q[st]), __builtin_bit_cast(pr_bf16x8, raw), s, 0, 0, 0);
     }
   }
   return s;
@@ -363,12 +356,6 @@ struct RowsWave {
           hi[t][j] = (__bf16)p[t][j];
           lo[t][j] = (__bf16)(p[t][j] - (float)hi[t][j]);
         }
-      auto pair = [&](int j, int y) {  // elements 2 y and 2 y + 1 of key j, as bf16
-        const float scale = b.value_scale(j >> 2);
-        if constexpr (L::F8) return (unsigned)__builtin_bit_cast(unsigned, (y & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, true)
-                                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b.v[j][y >> 1], scale, false));
-        else return b.v[j][y];
-      };
       const bool guard = !whole && values_not_finite(b);
       unsigned w[8];
 #pragma unroll
@@ -388,7 +375,7 @@ struct RowsWave {
         } else {
           if ((e & 1) == 0) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = pair(j, e >> 1);
+            for (int j = 0; j < 8; ++j) w[j] = b.v[j][e >> 1];
           }
 #pragma unroll
           for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(w[2 * y + 1], w[2 * y], (e & 1) ? 0x07060302u : 0x05040100u);

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
     const bool whole = __all(all);
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      const pr_f32x4 st = rows_products<E, D, false>(k[t], qf);
+      const pr_f32x4 st = rows_products<E, D>(k[t], qf);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[r]));
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
       float sum = 0.f;
 #pragma unroll
       for (int y = 0; y < RT; ++y) {
-        const pr_f32x4 st = rows_products<E, D, false>(b.k[t], qf[y]);
+        const pr_f32x4 st = rows_products<E, D>(b.k[t], qf[y]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[y][r]));

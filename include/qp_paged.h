@@ -82,7 +82,7 @@ size_t qp_paged_workspace_bytes(const qp_layout* layout, int32_t n_seqs, int32_t
  * result and a flat pruned cache's [H_kv][capacity][d] (token_stride d, head_stride capacity * d) can all be the source.
  *   pos: position of row r of head h at pos[r * pos_token_stride + h * pos_head_stride] (pos_head_stride 0: one per token)
  *   source_format: QP_CACHE_SAME, rows in the layout's dtype (rounded as qp_topk_compact rounds if the pool is 8-bit), or
- *     QP_CACHE_FP8_E4M3, rows that are E4M3 bytes already (8-bit pools only; strides then count bytes)
+ *     QP_CACHE_FP8_E4M3, rows that are E4M3 bytes already (8-bit pools without scales only; strides then count bytes)
  * The entries' weights, if the pool has them, become 0. */
 qp_status qp_paged_append(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, const void* k,
                           const void* v, int64_t token_stride, int64_t head_stride, const int32_t* pos,
@@ -99,7 +99,8 @@ typedef struct {
 
 /* qp_paged_append of keys that are not rotated yet (a plain projection's): pairs (i, i + head_dim / 2) of every key are turned by
  * pos * frequency on the way, and so are the queries of the same rows, if given. Angles as exact as f32 holds their sines and cosines,
- * f32 arithmetic, one rounding, to the pool's type (8-bit codes too) or, queries, the layout's.
+ * f32 arithmetic, one rounding, to the pool's type (8-bit codes too) or, queries, the layout's. Positions up to 2^26 in
+ * size; of larger ones the angles' last bits are lost.
  *   k, v: as in qp_paged_append (token_stride, head_stride in elements; rows of the layout's dtype)
  *   q_or_null: query head h of row r at q + (r * q_token_stride + h * q_head_stride), 16-byte aligned rows; q_out [n_rows][H_q][d], which
  *     may be q itself where that is dense. Rows of nobody are left as they were; both NULL: keys and values only

@@ -161,7 +161,9 @@ struct PagedTileArgs : AttendArgs {
   int chunk;       // filled per workgroup
 };
 // The same over a pool whose blocks of 16 entries have scales, and where a row sees a window of entries and the sequence's first ones: a row
-// block then leaves out the tiles between the two (RowsGap), and counts tiles without them.
+// block then leaves out the tiles between the two (RowsGap), and counts tiles without them. Four questions of up to 300 tokens of the 7B heads over up
+// to 46,125 entries: 8-bit 496 us, with scales 512 to 527 (where 600 is added to one channel of all keys, and references move more often); neither
+// their loads nor the registers that hold them explain the difference: fewer or earlier ones change nothing. In a window of 8,192 and 100 first entries, bf16: 148.
 template <bool SCALED, bool WINDOW>
 struct PagedTileArgsOf : PagedTileArgs {
   int span;  // keys in a row block's own count that a sequence has at most

@@ -13,6 +13,12 @@
 //   moves only when a logit exceeds it by 2^8, so that most blocks exchange nothing between lanes. Numerators are rounded to bf16
 //   twice (their value, and what that lost), so that 16-bit results differ from exact ones by their own rounding: the second
 //   product is hidden behind the loads. Denominators are summed from the unrounded ones.
+// What the vector unit does for a block of keys counts as soon as two row tiles meet 8-bit entries: it, not HBM, set the time of four tokens of 16
+// sequences over up to 32,768 entries (163 us) until masks were left to the blocks that need them, the products' chains were put side by side, and
+// two keys' bytes were paired before they are widened (141 us, a copy's rate).
+// Windows: a row tile's workgroups walk the first entries and its tokens' windows as one axis without what lies between (RowsGap), each unit by
+// workgroups of its own. us with the batch's blocks dealt evenly, as above / so: four tokens of 16 sequences of the 72B heads, window
+// 2,000, 8-bit with scales 46 / 37 (31 now), of 64 112 / 87; one token of 32 of the 7B heads, window 4,096, 63 / 59 (57 now).
 #include "paged_rows.h"
 
 #include <algorithm>
@@ -38,10 +44,9 @@ struct PagedOut {
   int2* info;      // [units]: first share of a unit and the shares that have blocks of it
 };
 
-// Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles spill 13 registers in front of and behind
-// the loop over the keys, not in it. Of bf16 heads of 128 one has the registers to itself: squeezed into half of them its results and
-// addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26. Of f32 heads of 128 too, and two row tiles spill 28
-// registers all the same, two of them in the loop too.
+// Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles fill the registers (with scales 4 of them spill, around
+// the loop over the keys). Of bf16 heads of 128 one has the registers to itself: squeezed into half of them its results and
+// addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26. Of f32 heads of 128 too.
 template <typename E, int D>
 constexpr int pr_waves() { return D == 64 || sizeof(E) == 1 ? 2 : 1; }
 
@@ -396,7 +401,7 @@ static long long merge_blocks(const PagedArgs& a, const PagedPlan& p) {
 }
 
 // Stacked rows above which bf16 heads of 128 take the tile kernel (attend_mfma.hip), and what its 32-bit arithmetic takes. A workgroup
-// for few rows holds 32; more of them take the entries once for each 32. us few rows / tiles, 7B heads, one sequence over 46,125
+// for few rows holds 32; more of them take the entries once for each 32. us few rows (before masks went behind a branch there) / tiles, 7B heads, one sequence over 46,125
 // entries: 1 token 26.0 / 29.3, 4 (28 rows) 30.9 / 30.9, 5 45.7 / 31.9, 12 61.9 / 35.8; 72B heads 46.0 / 56.6, 49.7 / 58.3, 77.8 / 59.5,
 // 106.9 / 65.4. Of 16 sequences over up to 9,840 the tiles win later, 7B heads 57.8 / 78.7, 64.8 / 79.9, 8 tokens 75.6 / 82.1, 12
 // 94.1 / 86.4; 72B heads 95.2 / 111.0, 110.4 / 112.4, 135.2 / 116.6; over 8-bit pools of the 7B heads not up to 12 (68.3 / 90.0).
@@ -421,7 +426,8 @@ PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch
   const long long units = (long long)a.n_seqs * p.tiles, cus = device_cu_count();
   if (!tiled) {
     // One workgroup per compute unit, two over 8-bit pools, whose blocks are longer chains over half the bytes, as long as each has
-    // a block. us, equal shares of all entries / equal chunks of the longest sequence (1, 2 and 4 workgroups per compute unit): up to
+    // a block. us with the kernel as it was before masks went behind a branch (the first figure is 141 now, the second 76.5), equal
+    // shares of all entries / equal chunks of the longest sequence (1, 2 and 4 workgroups per compute unit): up to
     // four tokens of 16 sequences of the 72B heads over 8-bit pages of up to 32,768 entries 163 / 251, 180, 187; one token of 32
     // sequences of the 7B heads over up to 9,840 79.0 / 84.8, 89.8, 93.2, of one over 46,125 26.0 / 25.0, 27.6, 30.1.
     const int step = PR_NW * (dtype == QP_F32 ? 16 : 32);

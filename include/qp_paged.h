@@ -30,7 +30,7 @@
  * 448: keys of channels with large offsets saturate. Codes are floating-point themselves, so a finer scale would not make them more exact; a power of two
  * is exact wherever it is applied. An append gives a block the least scale that holds its finite values (infinities saturate, NaN stays) and never
  * a smaller one than the block's earlier entries have; where it grows, their codes are divided with it, exactly down to 2^-6 of the new
- * scale and rounded below. qp_paged_weigh and qp_paged_evict do not take such pools (UNSUPPORTED).
+ * scale and rounded below. Entries that qp_paged_evict moves join blocks of new neighbours, whose scale is the largest of theirs, their codes divided in the same way.
  */
 #ifndef QP_PAGED_H_
 #define QP_PAGED_H_
@@ -132,7 +132,7 @@ qp_status qp_paged_attend_window(const qp_layout* layout, const qp_paged_cache* 
                                  void* hip_stream);
 
 /* weight[j] of KV head h = (accumulate ? weight[j] : 0) + the sum of exp(scale * q.k_j - lse) over the sequence's new rows that
- * see j and the H_q / H_kv query heads of h, for every entry j < len[s]: with the lse that qp_paged_attend wrote for the same
+ * see j and the H_q / H_kv query heads of h, for every entry j < len[s]: with the lse that qp_paged_attend (not qp_paged_attend_window) wrote for the same
  * rows, the attention weight that the entry received. Rows of lse = -infinity add nothing. f32 arithmetic. cache->weight must
  * be there. workspace: may be NULL; calls of many rows over few entries deal the rows to several workgroups where it is given. */
 qp_status qp_paged_weigh(const qp_layout* layout, const qp_paged_cache* cache, const qp_paged_batch* batch, const void* q,

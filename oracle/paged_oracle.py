@@ -166,3 +166,23 @@ def append_scaled(k, v, k_size, pos, pool, batch, k_largest, store=fp8_e4m3_roun
             for j, row in zip(new, rows):
                 pool["pos"][page, :, j % p], pool["weight"][page, :, j % p] = pos[row], 0
     return pool
+
+
+def move_scaled(pool, table, kept, to_table):
+    """The pool with scales after the entries kept[s][h] of every sequence and head were moved to the pages of to_table: a block of them gets the
+    largest of their scales."""
+    pool = {name: x.copy() for name, x in pool.items()}
+    p = pool["k"].shape[2]
+    for s, heads in enumerate(kept):
+        for h, entries in enumerate(heads):
+            for block in range(-(-len(entries) // 16)):
+                old = entries[16 * block:16 * block + 16]
+                page, slot = np.asarray(table[s])[old // p], old % p
+                to, at = to_table[s][16 * block // p], 16 * block % p
+                for name in ("k", "v"):
+                    scales = pool[name + "_scale"][page, h, slot // 16]
+                    pool[name + "_scale"][to, h, at // 16] = scales.max()
+                    pool[name][to, h, at:at + len(old)] = fp8_e4m3_round(pool[name][page, h, slot] * (scales / scales.max())[:, None])
+                for name in ("pos", "weight"):
+                    pool[name][to, h, at:at + len(old)] = pool[name][page, h, slot]
+    return pool

@@ -206,7 +206,6 @@ qp_status qp_paged_weigh(const qp_layout* L, const qp_paged_cache* cache, const 
   const qp_status st = check(L, cache, batch, true, &a);
   if (st != QP_OK) return st;
   if (a.weight == nullptr || !aligned(q, 16) || !aligned(lse, 4) || bad_workspace(workspace)) return QP_ERR_INVALID_ARG;
-  if (a.fp8 == QP_CACHE_FP8_E4M3_SCALED) return QP_ERR_UNSUPPORTED;
   return finish(qp::launch_paged_weigh(a, L->dtype, L->head_dim, q, lse, accumulate != 0, workspace, workspace_bytes,
                                        (hipStream_t)hip_stream));
 }
@@ -222,7 +221,7 @@ qp_status qp_paged_evict(const qp_layout* L, const qp_paged_cache* cache, const 
   if (!aligned(to_table, 4) || !aligned(to_len, 4) || to_pages <= 0 || (kept_or_null != nullptr && !aligned(kept_or_null, 4)) ||
       bad_workspace(workspace))
     return QP_ERR_INVALID_ARG;
-  if (keep > kMaxLen || a.fp8 == QP_CACHE_FP8_E4M3_SCALED) return QP_ERR_UNSUPPORTED;
+  if (keep > kMaxLen) return QP_ERR_UNSUPPORTED;
   if (((int64_t)to_pages << a.page_shift) < keep) return QP_ERR_CAPACITY;
   if (workspace == nullptr || workspace_bytes < evict_bytes(a.n_seqs, a.h_kv, keep, a.max_len)) return QP_ERR_CAPACITY;
   qp::PagedEvict e{};

@@ -5,7 +5,7 @@
 // evict    two launches. evict_select_kernel: one workgroup per (sequence, head) finds the threshold among order-preserving keys
 //          (select_threshold) and lists the entries that stay, in order. evict_move_kernel: many workgroups copy the listed rows,
 //          which is where the bytes are (4 rows of head_dim per kept entry against 4 bytes per entry for the selection).
-#include "append.h"
+#include "codes.h"
 #include "paged.h"
 #include "select.h"
 
@@ -400,16 +400,95 @@ __global__ __launch_bounds__(EM_THREADS) void evict_move_kernel(PagedArgs a, Pag
   }
 }
 
+// The move into a pool with scales: a wavefront has a block of 16 of the kept entries, which share scales that fit all of them: the largest of
+// their old ones. 8 lanes have a row.
+__global__ __launch_bounds__(EM_THREADS) void evict_move_scaled_kernel(PagedArgs a, PagedEvict e, int blocks_per_head) {
+  constexpr int NW = EM_THREADS / 64, LPR = 8, PASSES = 2;
+  const int lane = threadIdx.x & 63, sub = lane % LPR;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sh = blockIdx.x / blocks_per_head, b = (blockIdx.x - sh * blocks_per_head) * NW + wave;
+  const int s = sh / a.h_kv, h = sh - s * a.h_kv;
+  const int mask = (1 << a.page_shift) - 1;
+  const int32_t* const kept = e.kept + (size_t)sh * e.keep;
+  const long long x0 = (long long)b * PAGED_BLOCK;
+  if (x0 >= e.keep) return;
+  const int first = (int)x0, t = e.to_table[(size_t)s * e.to_pages + (first >> a.page_shift)];
+  const bool there = paged_page_ok(t, a.n_pages);  // no destination: the entries are dropped
+  const size_t to = paged_row(there ? t : 0, h, first & mask, a.h_kv, a.page_shift);
+  int from[PASSES], ke = PAGED_SCALE_MIN, ve = PAGED_SCALE_MIN, k_exp[PASSES], v_exp[PASSES], pos[PASSES];
+  float w[PASSES];
+  u32x4 kk[PASSES], vv[PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    const int x = first + p * (64 / LPR) + lane / LPR;
+    from[p] = x < e.keep ? kept[x] : -1;
+    if (h == 0 && sub == 0 && x < e.keep) {  // the new length is where the list ends, as in evict_move_kernel
+      if (from[p] < 0 && (x == 0 || kept[x - 1] >= 0)) e.to_len[s] = x;
+      if (from[p] >= 0 && x == e.keep - 1) e.to_len[s] = e.keep;
+    }
+    if (from[p] < 0) continue;
+    const int page = a.table[(size_t)s * a.table_pages + (from[p] >> a.page_shift)];
+    if (!there || !paged_page_ok(page, a.n_pages)) {
+      from[p] = -1;
+      continue;
+    }
+    const size_t row = paged_row(page, h, from[p] & mask, a.h_kv, a.page_shift);
+    kk[p] = *(const u32x4*)((const unsigned char*)a.k + row * (LPR * 16) + sub * 16);
+    vv[p] = *(const u32x4*)((const unsigned char*)a.v + row * (LPR * 16) + sub * 16);
+    k_exp[p] = scale_exponent(a.k_scale[row >> 4], PAGED_SCALE_MIN, PAGED_SCALE_MAX);
+    v_exp[p] = scale_exponent(a.v_scale[row >> 4], PAGED_SCALE_MIN, PAGED_SCALE_MAX);
+    ke = max(ke, k_exp[p]);
+    ve = max(ve, v_exp[p]);
+    if (sub == 0) {
+      pos[p] = a.pos[row];
+      w[p] = a.weight[row];
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    ke = max(ke, __shfl_xor(ke, o, 64));
+    ve = max(ve, __shfl_xor(ve, o, 64));
+  }
+  if (!__any(from[0] >= 0 || from[1] >= 0)) return;
+  if (lane == 0) {
+    a.k_scale[to >> 4] = pow2f(ke);
+    a.v_scale[to >> 4] = pow2f(ve);
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (from[p] < 0) continue;
+    const size_t row = to + p * (64 / LPR) + lane / LPR;
+    const float kb = pow2f(max(k_exp[p] - ke, -126)), vb = pow2f(max(v_exp[p] - ve, -126));
+    if (k_exp[p] < ke) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) kk[p][c] = shrink4(kk[p][c], kb);
+    }
+    if (v_exp[p] < ve) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vv[p][c] = shrink4(vv[p][c], vb);
+    }
+    *(u32x4*)((unsigned char*)a.k + row * (LPR * 16) + sub * 16) = kk[p];
+    *(u32x4*)((unsigned char*)a.v + row * (LPR * 16) + sub * 16) = vv[p];
+    if (sub == 0) {
+      a.pos[row] = pos[p];
+      a.weight[row] = w[p];
+    }
+  }
+}
+
 template <int LPR>
 static bool evict_as(const PagedArgs& a, const PagedEvict& e, hipStream_t s) {
   constexpr int ROWS = EM_THREADS / LPR * EM_UNROLL;
-  const long long per = ((long long)e.keep + ROWS - 1) / ROWS;
+  const bool scaled = a.fp8 == QP_CACHE_FP8_E4M3_SCALED;
+  const int rows = scaled ? EM_THREADS / 64 * PAGED_BLOCK : ROWS;
+  const long long per = ((long long)e.keep + rows - 1) / rows;
   const long long heads = (long long)a.n_seqs * a.h_kv;
   if (per * heads * EM_THREADS > PAGED_MAX_THREADS || heads * SEL_THREADS > PAGED_MAX_THREADS) return false;
   const dim3 grid((unsigned)heads), block(SEL_THREADS);
   if (e.keys == nullptr) hipLaunchKernelGGL(evict_select_kernel<true>, grid, block, 0, s, a, e);
   else hipLaunchKernelGGL(evict_select_kernel<false>, grid, block, 0, s, a, e);
-  hipLaunchKernelGGL(evict_move_kernel<LPR>, dim3((unsigned)(per * heads)), dim3(EM_THREADS), 0, s, a, e, (int)per);
+  if (scaled) hipLaunchKernelGGL(evict_move_scaled_kernel, dim3((unsigned)(per * heads)), dim3(EM_THREADS), 0, s, a, e, (int)per);
+  else hipLaunchKernelGGL(evict_move_kernel<LPR>, dim3((unsigned)(per * heads)), dim3(EM_THREADS), 0, s, a, e, (int)per);
   return true;
 }
 

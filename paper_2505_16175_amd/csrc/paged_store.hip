@@ -14,7 +14,7 @@
 // 8-bit pages without 65.5, bf16 82; out of tensors of their own 65.6, 63.0, 80.0, as fast as qp_paged_append copies them.
 //   Before: half rows per load (36.1, 71.0), four heads' rows loaded ahead of the first store (42, 90: half the wavefronts), two heads' in turn (44, 81),
 // four blocks of entries per workgroup, one after the other (42, 77), workgroups of 8 blocks (39, 111).
-#include "append.h"
+#include "codes.h"
 #include "paged.h"
 
 #include <algorithm>
@@ -27,19 +27,12 @@ constexpr int PS_WAVES = 4;
 constexpr int PS_THREADS = PS_WAVES * 64;
 constexpr int PS_BLOCK = PAGED_BLOCK;
 
-// 4 f32 values as E4M3 codes: nearest, ties to even; what is beyond +-448 saturates, NaN stays.
-__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
-  auto in = [](float x) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -448.f), 448.f); };
-  const unsigned lo = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
-  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), (int)lo, true);
-}
 // Two values as bf16, nearest, ties to even; NaN stays NaN.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
 // The 16 bytes of the lane D lanes away (lane ^ D).
 template <int D>
@@ -160,7 +153,7 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
         e = max(e, PAGED_SCALE_MIN);
         float* const scale = (is_v ? a.v_scale : a.k_scale) + (row0 >> 4);
         if (!FULL && e0 < q.base) {  // earlier entries of the block: its scale may only grow, and their codes go with it
-          const int was = min(max((int)((__float_as_uint(*scale) >> 23) & 255u) - 127, PAGED_SCALE_MIN), PAGED_SCALE_MAX);
+          const int was = scale_exponent(*scale, PAGED_SCALE_MIN, PAGED_SCALE_MAX);
           e = __builtin_amdgcn_readfirstlane(max(e, was));
           if (e > was) {
             const float shrink = pow2f(max(was - e, -126));
@@ -170,11 +163,7 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
               if (i0 + t >= 0) continue;
               uint2* const at = (uint2*)(pool + (row0 + t) * D + sub * OUT_BYTES);
               uint2 c = *at;
-              auto smaller = [&](unsigned w) {
-                return codes4(__builtin_amdgcn_cvt_f32_fp8(w, 0) * shrink, __builtin_amdgcn_cvt_f32_fp8(w, 1) * shrink,
-                              __builtin_amdgcn_cvt_f32_fp8(w, 2) * shrink, __builtin_amdgcn_cvt_f32_fp8(w, 3) * shrink);
-              };
-              c.x = smaller(c.x), c.y = smaller(c.y);
+              c.x = shrink4(c.x, shrink), c.y = shrink4(c.y, shrink);
               *at = c;
             }
           }

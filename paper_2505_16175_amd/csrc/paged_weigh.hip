@@ -47,14 +47,16 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
   const int mask = (1 << a.page_shift) - 1;
 
   pr_u32x4 k[KT][L::KL];
+  float scale[KT];  // of the tiles' codes: their products with the queries are multiplied, exactly, instead
   int page[KT];
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
     const int key = key0 + 16 * t;
     page[t] = key < q.len ? __builtin_amdgcn_readfirstlane(a.table[(size_t)s * a.table_pages + (key >> a.page_shift)]) : -1;
     if (!paged_page_ok(page[t], a.n_pages)) page[t] = -1;
-    const size_t at = paged_row(max(page[t], 0), h, key & mask, a.h_kv, a.page_shift) * L::ROWB;
-    rows_load_k<E, D>((const unsigned char*)a.k + at, l16, g, k[t]);
+    const size_t row = paged_row(max(page[t], 0), h, key & mask, a.h_kv, a.page_shift);
+    rows_load_k<E, D>((const unsigned char*)a.k + row * L::ROWB, l16, g, k[t]);
+    scale[t] = L::SCALED ? a.k_scale[row >> 4] : 1.f;
   }
   float w[KT];
   float* to[KT];  // group g stores tile g: what was there is requested with the keys
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
       const pr_f32x4 st = rows_products<E, D>(k[t], qf);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[r]));
+        const float p = __builtin_amdgcn_exp2f(fmaf(st[r], L::SCALED ? c2 * scale[t] : c2, neg[r]));
         w[t] += whole || key0 + 16 * t + l16 <= lim[r] ? p : 0.f;
       }
     }
@@ -139,10 +141,12 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
     pr_u32x4 k[L::TILES][L::KL];
     float* to;     // group t: the entry of tile t that this lane stores, nullptr: none
     float before;
+    float scales;  // SCALED: that of tile t's codes in lane t, see RowsBlock
   };
   auto load = [&](Block& b, int key0) {
     b.to = nullptr;
     b.before = 0.f;
+    size_t rows[L::TILES];
 #pragma unroll
     for (int t = 0; t < L::TILES; ++t) {
       const int key = key0 + 16 * t;
@@ -150,9 +154,11 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
       const int page = __builtin_amdgcn_readlane(list, ((key < end ? key : key0) >> a.page_shift) - page0);
       const bool ok = paged_page_ok(page, a.n_pages);
       const size_t row = paged_row(ok ? page : 0, h, key & mask, a.h_kv, a.page_shift);
+      rows[t] = row;
       rows_load_k<E, D>((const unsigned char*)a.k + row * L::ROWB, l16, g, b.k[t]);
       if (g == t && ok && key + l16 < end) b.to = a.weight + row + l16;
     }
+    if constexpr (L::SCALED) b.scales = a.k_scale[((lane & 1) ? rows[L::TILES - 1] : rows[0]) >> 4];
     if (accumulate && b.to != nullptr) b.before = *b.to;
   };
   const int n_rows = q.n * r_heads;  // 16 RT at most
@@ -194,13 +200,14 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
     float w = 0.f;
 #pragma unroll
     for (int t = 0; t < L::TILES; ++t) {
-      float sum = 0.f;
+      float sum = 0.f, c = c2;
+      if constexpr (L::SCALED) c *= __uint_as_float((unsigned)__builtin_amdgcn_readlane(__float_as_uint(b.scales), t));
 #pragma unroll
       for (int y = 0; y < RT; ++y) {
         const pr_f32x4 st = rows_products<E, D>(b.k[t], qf[y]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[y][r]));
+          const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c, neg[y][r]));
           sum += whole || key0 + 16 * t + l16 <= lim[y][r] ? p : 0.f;
         }
       }
@@ -242,7 +249,7 @@ __device__ __forceinline__ void weigh_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-template <bool F8>
+template <bool F8, bool SCALED>
 __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, WeighTiles o) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ __attribute__((aligned(16))) float neg[WT_ROWS];  // -lse of the segment's rows, base 2
@@ -278,11 +285,12 @@ __global__ __launch_bounds__(WT_NW * 64, 3) void weigh_tile_kernel(PagedArgs a, 
     if (g == b) mine_at = at, mine = ok && key < q.len;
     first_row[b] = paged_clamp(key - q.base, 0, q.n) * r_heads;
     const unsigned char* p = (const unsigned char*)a.k + at * ROWB;
+    const float scale = SCALED && ok ? a.k_scale[at >> 4] : 1.f;
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
       if constexpr (F8) {
         const uint2 raw = *(const uint2*)(p + 32 * st + 8 * g);
-        k[b][st] = pr_widen8(raw.x, raw.y);
+        k[b][st] = pr_widen8(raw.x, raw.y, scale);
       } else {
         k[b][st] = *(const pr_u32x4*)(p + 64 * st + 16 * g);
       }
@@ -469,7 +477,7 @@ size_t paged_weigh_workspace_bytes(int n_seqs, int h_q, int h_kv, int max_new, i
   return splits > 1 ? splits * per : 0;
 }
 
-template <bool F8>
+template <bool F8, bool SCALED>
 static bool weigh_tiles_as(const PagedArgs& a, const void* q, const float* lse, int accumulate, void* scratch, size_t scratch_bytes,
                            hipStream_t s) {
   const long long blocks = weigh_blocks(a.n_seqs, a.h_kv, a.max_len);
@@ -477,7 +485,7 @@ static bool weigh_tiles_as(const PagedArgs& a, const void* q, const float* lse, 
   if (scratch != nullptr)
     o.splits = weigh_splits(blocks, (long long)a.max_new * (a.h_q / a.h_kv), weigh_per_split(a.n_seqs, a.h_kv, a.max_len), scratch_bytes);
   if (blocks * o.splits * WT_NW * 64 > PAGED_MAX_THREADS) return false;
-  hipLaunchKernelGGL((weigh_tile_kernel<F8>), dim3((unsigned)(blocks * o.splits)), dim3(WT_NW * 64), WT_LDS, s, a, o);
+  hipLaunchKernelGGL((weigh_tile_kernel<F8, SCALED>), dim3((unsigned)(blocks * o.splits)), dim3(WT_NW * 64), WT_LDS, s, a, o);
   if (o.splits > 1) {
     const int per = (a.max_len + WA_THREADS - 1) / WA_THREADS;
     hipLaunchKernelGGL(weigh_add_kernel, dim3((unsigned)((long long)per * a.n_seqs * a.h_kv)), dim3(WA_THREADS), 0, s, a, o, per);
@@ -510,9 +518,11 @@ static bool weigh_as(const PagedArgs& a, const void* q, const float* lse, int ac
 bool launch_paged_weigh(const PagedArgs& a, int dtype, int d, const void* q, const float* lse, int accumulate, void* scratch,
                         size_t scratch_bytes, hipStream_t s) {
   if (weigh_tiled(a, dtype, d))
-    return a.fp8 ? weigh_tiles_as<true>(a, q, lse, accumulate, scratch, scratch_bytes, s)
-                 : weigh_tiles_as<false>(a, q, lse, accumulate, scratch, scratch_bytes, s);
+    return a.fp8 == QP_CACHE_FP8_E4M3_SCALED ? weigh_tiles_as<true, true>(a, q, lse, accumulate, scratch, scratch_bytes, s)
+           : a.fp8                           ? weigh_tiles_as<true, false>(a, q, lse, accumulate, scratch, scratch_bytes, s)
+                                             : weigh_tiles_as<false, false>(a, q, lse, accumulate, scratch, scratch_bytes, s);
   if (dtype == QP_F32) return d == 64 ? weigh_as<float, 64>(a, q, lse, accumulate, s) : weigh_as<float, 128>(a, q, lse, accumulate, s);
+  if (a.fp8 == QP_CACHE_FP8_E4M3_SCALED) return weigh_as<ScaledCode, 128>(a, q, lse, accumulate, s);
   if (a.fp8) return weigh_as<uint8_t, 128>(a, q, lse, accumulate, s);
   return d == 64 ? weigh_as<bf16_t, 64>(a, q, lse, accumulate, s) : weigh_as<bf16_t, 128>(a, q, lse, accumulate, s);
 }

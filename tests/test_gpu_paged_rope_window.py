@@ -182,6 +182,53 @@ def test_scales_of_any_size():
                 check_plain(sc, *attend(sc), plain(sc), f"keys 2^{e}")
 
 
+@pytest.mark.parametrize("layout,page,lens,new,missing", [
+    (L7, 16, [700, 33, 32, 31, 1, 0], [1, 1, 1, 1, 1, 0], []), (L7, 64, [1000, 999, 65], [4, 2, 1], []), (L72, 32, [513, 40], [2, 1], [(0, 12), (1, 1)]),
+    (WIDE, 64, [100, 260], [1, 3], []), (L7, 64, [3, 0, 70], [9, 4, 75], []), (L7, 128, [600, 300, 129], [40, 7, 1], []), (L7, 256, [2000], [300], []),
+    (L72, 64, [700, 640, 300], [60, 64, 3], [(0, 0), (0, 10), (1, 3), (1, 4), (2, 4)])])
+def test_weigh_over_scales(layout, page, lens, new, missing):
+    sc = scaled_pool(Scene(layout, page, lens, new, seed=page + len(lens), missing=missing), seed=len(lens))
+    _, lse = attend(sc)
+    values_pool = P.dequantised(dict(sc.pool(), k_scale=to_f64(sc.cache.k_scale), v_scale=to_f64(sc.cache.v_scale)))
+    size = np.nan_to_num(P.attend(to_f64(sc.q), values_pool, sc.oracle_batch, sc.scale)[3]).max() + np.abs(np.where(np.isfinite(to_f64(lse)), to_f64(lse), 0)).max()
+    # as test_gpu_paged.py: logits, and one rounding more, of the scale's product with the softmax scale: none, a power of two
+    e = (sc.d + 16) * U * size + 2.0 ** -22 + (max(new + [1]) * (sc.h_q // sc.h_kv) + 4) * U
+    for accumulate in (True, False):
+        for ws in (sc.ws, None):
+            before = dict(values_pool, weight=to_f64(sc.cache.weight))
+            B.paged_weigh(sc.layout, sc.cache, sc.batch, sc.q.to(DEV), lse, accumulate, ws)
+            torch.cuda.synchronize()
+            want, added = P.weigh(to_f64(sc.q), to_f64(lse), before, sc.oracle_batch, sc.scale, accumulate)
+            assert (np.abs(to_f64(sc.cache.weight) - want) <= added * e + 2 * U * np.abs(want) + 1e-37).all()
+
+
+@pytest.mark.parametrize("layout,page,lens,keep,first,last,missing", [
+    (L7, 64, [700, 300, 65], 200, 4, 16, []), (L7, 16, [1, 0, 17], 8, 1, 1, []), (L72, 32, [513, 100], 99, 3, 50, [(0, 7)]), (ODD, 256, [1000], 1000, 4, 4, []),
+    (L7, 16, [50000, 40], 9, 2, 3, []), (WIDE, 128, [400, 129], 129, 0, 129, [(0, 1)])])
+def test_evict_over_scales(layout, page, lens, keep, first, last, missing):
+    """The entries of most weight in other pages: what they stand for, but for the rounding of those that join a block of larger scales."""
+    pages = -(-keep // page)
+    sc = scaled_pool(Scene(layout, page, lens, [0] * len(lens), seed=keep, missing=missing, spare_pages=len(lens) * (pages + 1) + 2), seed=1, spread=6)
+    used = set(x for row in sc.table.tolist() for x in row)
+    free = [p for p in range(sc.cache.c.n_pages) if p not in used]
+    to = torch.tensor([[free.pop() for _ in range(pages)] + [-1] for _ in lens], dtype=torch.int32)
+    before = dict(sc.pool(), k_scale=to_f64(sc.cache.k_scale), v_scale=to_f64(sc.cache.v_scale))
+    to_len, kept = i32([-1] * len(lens)), torch.full((len(lens), sc.h_kv, keep), 99, dtype=torch.int32, device=DEV)
+    ws = B.make_paged_workspace(sc.layout, sc.batch, keep, page)
+    B.paged_evict(sc.layout, sc.cache, sc.batch, keep, first, last, to.to(DEV), to_len, kept, ws)
+    torch.cuda.synchronize()
+    lists = P.evict(before, sc.table.tolist(), lens, keep, first, last)
+    lists = [lists[s * sc.h_kv:(s + 1) * sc.h_kv] for s in range(len(lens))]
+    assert to_len.tolist() == [len(x[0]) for x in lists]
+    for s in range(len(lens)):
+        for h in range(sc.h_kv):
+            np.testing.assert_array_equal(kept[s, h].cpu().numpy(), np.concatenate([lists[s][h], np.full(keep - len(lists[s][h]), -1)]))
+    want = P.move_scaled(before, sc.table.tolist(), lists, to.tolist())
+    got = dict(sc.pool(), k_scale=to_f64(sc.cache.k_scale), v_scale=to_f64(sc.cache.v_scale))
+    for name in want:
+        np.testing.assert_array_equal(got[name], want[name], err_msg=name)
+
+
 # ---- windows ----
 
 WINDOWS = [(1, 0), (1, 1), (2, 4), (15, 0), (16, 16), (17, 1), (31, 33), (64, 0), (65, 64), (100, 4), (127, 130), (300, 17), (5000, 0), (2 ** 31 - 1, 2 ** 31 - 1)]
@@ -568,9 +615,6 @@ def test_refusals_of_the_binding():
         B.paged_attend_window(sc.layout, sc.cache, sc.batch, 5, 0, q_out[:, 1:], out)
     scaled = B.PagedCache(sc.layout, 4, 64, fmt=SCALED)
     assert scaled.k_scale.shape == (4, 4, 4) and (scaled.v_scale == 1).all()
-    batch = B.PagedBatch(i32([[1, 0]]), i32([70]), i32([0, sc.n_rows]), sc.n_rows)
-    with pytest.raises(B.QPError):
-        B.paged_weigh(sc.layout, scaled, batch, q_out, lse)
     with pytest.raises(ValueError):
         B.PagedCache(sc.layout, 4, 64, k_scale=scaled.k_scale)
     with pytest.raises(ValueError):

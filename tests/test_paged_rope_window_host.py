@@ -58,7 +58,7 @@ NEW = ("append", "rope", "attend", "window")
 @pytest.mark.parametrize("change,status,calls", [
     (dict(k_scale=None), INV, ALL), (dict(v_scale=None), INV, ALL), (dict(k_scale=FAKE + 2), INV, ALL), (dict(v_scale=FAKE + 1), INV, ALL),
     (dict(format=3), INV, ALL), (dict(format=-1), INV, ALL), (dict(dtype="f32"), UNS, ALL), (dict(d=64, section=(8, 12, 12)), UNS, ALL),
-    (dict(), UNS, ("weigh", "evict")), (dict(source=1), UNS, ("append",)),
+    (dict(source=1), UNS, ("append",)),
     (dict(page_tokens=8), UNS, NEW), (dict(n_rows=0), INV, NEW), (dict(max_new=0), INV, NEW), (dict(row_start=None), INV, NEW),
     (dict(len=None), INV, NEW), (dict(n_seqs=0), INV, NEW), (dict(max_len=(1 << 30) + 1), UNS, NEW),
     (dict(rope=False), INV, ("rope",)), (dict(axes=None), INV, ("rope",)), (dict(axes=FAKE + 2), INV, ("rope",)), (dict(axis_stride=-1), INV, ("rope",)),
@@ -92,7 +92,7 @@ def test_valid_calls_reach_the_launch():
                    dict(format=0, dtype="f32", d=64, section=(32, 0, 0), axis_stride=0), dict(window=2 ** 31 - 1, n_sink=2 ** 31 - 1), dict(weight=None),
                    dict(max_new=300, n_rows=900, n_seqs=3)):
         got = _call(**change)
-        assert {got[name] for name in NEW} == {hip}, change
+        assert {got[name] for name in (NEW if change.get("weight", 1) is None else ALL)} == {hip}, change
     assert _call(q=None, out=None)["rope"] == hip                 # keys and values only
     assert _call(format=0, k_scale=None, v_scale=None)["attend"] == hip
 
@@ -146,3 +146,12 @@ def test_oracle_turns_pairs_by_their_axis():
     got = P.turn(x, axes, 100.0, (1, 1, 1))[0, 0]
     a = 2 * 100 ** (-4 / 6)
     np.testing.assert_allclose(got, [np.cos(1), 0, 2 * np.cos(a), np.sin(1), 0, 2 * np.sin(a)])
+
+
+def test_oracle_moves_entries_of_different_scales_into_one_block():
+    k = np.zeros((3, 1, 16, 1))
+    k[0, 0, :2, 0], k[1, 0, 0, 0] = [448.0, 2.0 ** -9], 3.0
+    scale = np.array([1.0, 8.0, 64.0]).reshape(3, 1, 1)
+    pool = dict(k=k, v=k.copy(), pos=np.arange(48).reshape(3, 1, 16), weight=np.ones((3, 1, 16)), k_scale=scale, v_scale=scale.copy())
+    got = P.move_scaled(pool, [[0, 1]], [[np.array([0, 1, 16])]], [[2]])
+    assert got["k_scale"][2, 0, 0] == 8.0 and got["k"][2, 0, :3, 0].tolist() == [56.0, 0.0, 3.0] and got["pos"][2, 0, :3].tolist() == [0, 1, 16]

@@ -26,7 +26,8 @@
  * it may be there once: two writers of one entry race, and only its value is then unspecified.
  * Supported: dtype f32 or bf16, head_dim 64 or 128, pages of 16, 32, 64, 128 or 256 tokens; 8-bit pools (E4M3) as in qp.h.
  *   QP_CACHE_FP8_E4M3_SCALED: an 8-bit pool (bf16 layouts of head_dim 128) whose entries j / 16 of a sequence share a scale per KV head, one
- * for keys and one for values: an element is code * scale, scale a power of two from 2^-117 to 2^120. E4M3 codes alone hold magnitudes from 2^-9 to
+ * for keys and one for values: an element is code * scale, scale a power of two from 2^-117 to 2^120 (at which codes beyond
+ * +-240 are infinities, and appends saturate at 240). E4M3 codes alone hold magnitudes from 2^-9 to
  * 448: keys of channels with large offsets saturate. Codes are floating-point themselves, so a finer scale would not make them more exact; a power of two
  * is exact wherever it is applied. An append gives a block the least scale that holds its finite values (infinities saturate, NaN stays) and never
  * a smaller one than the block's earlier entries have; where it grows, their codes are divided with it, exactly down to 2^-6 of the new

@@ -136,6 +136,11 @@ def block_exponent(x, largest):
     return e
 
 
+def codes_that_fit(x, e):
+    """Scaled values as far as codes can hold them: at a scale of 2^120 those beyond 240 would stand for more than f32 holds."""
+    return np.clip(x, -240.0, 240.0) if e == 120 else x
+
+
 def append_scaled(k, v, k_size, pos, pool, batch, k_largest, store=fp8_e4m3_round):
     """The pool with scales after the new rows: entry by entry, which gives a block the same scale as all at once, and its earlier entries'
     codes as if the block's scale had been known (one rescaling of what was there before the call). k_size: rows whose magnitudes the keys' scales
@@ -162,7 +167,7 @@ def append_scaled(k, v, k_size, pos, pool, batch, k_largest, store=fp8_e4m3_roun
                         slots = [j % p for j in old]
                         pool[name][page, h, slots] = fp8_e4m3_round(pool[name][page, h, slots] * 2.0 ** (was - e))
                     scale[page, h, at // 16] = 2.0 ** e
-                    pool[name][page, h, [j % p for j in new]] = store(x[rows, h] * 2.0 ** -e)
+                    pool[name][page, h, [j % p for j in new]] = store(codes_that_fit(x[rows, h] * 2.0 ** -e, e))
             for j, row in zip(new, rows):
                 pool["pos"][page, :, j % p], pool["weight"][page, :, j % p] = pos[row], 0
     return pool

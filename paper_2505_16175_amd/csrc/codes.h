@@ -6,9 +6,9 @@
 
 namespace qp {
 
-// 4 f32 values as E4M3 codes: nearest, ties to even; what is beyond +-448 saturates, NaN stays.
-__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d) {
-  auto in = [](float x) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -448.f), 448.f); };
+// 4 f32 values as E4M3 codes: nearest, ties to even; what is beyond +-most saturates, NaN stays.
+__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, float most = 448.f) {
+  auto in = [=](float x) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -most), most); };
   const unsigned lo = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(in(a), in(b), 0, false);
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(in(c), in(d), (int)lo, true);
 }

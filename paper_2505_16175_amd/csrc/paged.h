@@ -7,8 +7,10 @@
 namespace qp {
 
 constexpr int PAGED_BLOCK = 16;  // entries that share a scale
-// Exponents of the scales: from the least whose smallest code is a normal f32 and bf16 value to the least that holds the largest f32.
+// Exponents of the scales: from the least whose smallest code is a normal f32 and bf16 value to the largest of which some codes stand for values
+// that no smaller one holds: of 2^120 those up to 240. The next, 256, would be 2^128, which f32 and bf16 hold as infinity, as 448 * 2^120 is.
 constexpr int PAGED_SCALE_MIN = -117, PAGED_SCALE_MAX = 120;
+constexpr float PAGED_SCALE_MAX_CODE = 240.f;
 
 struct PagedArgs {
   void* k;         // [n_pages][h_kv][1 << page_shift][d]

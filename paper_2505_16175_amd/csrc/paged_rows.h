@@ -243,9 +243,15 @@ struct RowsWave {
   }
 
   // Whether some value of the block is an infinity or NaN: an element of which the exponent (of E4M3: everything but the sign) is all ones, to
-  // which its least bit is added and makes the next.
+  // which its least bit is added and makes the next. At the largest scale every code from 256 on stands for an infinity: such blocks, in which
+  // hardly anything else is, count as if they had one.
   __device__ __forceinline__ bool values_not_finite(const Block& b) const {
     constexpr unsigned ONES = L::F32 ? 0x7f800000u : L::F8 ? 0x7f7f7f7fu : 0x7f807f80u, LEAST = L::F32 ? 0x00800000u : L::F8 ? 0x01010101u : 0x00800080u;
+    if constexpr (L::SCALED) {
+#pragma unroll
+      for (int t = 0; t < L::TILES; ++t)
+        if (b.value_scale(t) >= 0x1p120f) return true;
+    }
     unsigned found = 0;
 #pragma unroll
     for (int j = 0; j < L::VK; ++j)

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
     constexpr bool FULL = decltype(full)::value;
     const bool is_q = item >= 2 * a.h_kv, is_v = !is_q && item >= a.h_kv;
     const int h = is_q ? item - 2 * a.h_kv : is_v ? item - a.h_kv : item;
-    float unscale = 1.f;
+    float unscale = 1.f, most_code = 448.f;
     const size_t row0 = FULL || stored ? paged_row(page, h, slot0, a.h_kv, a.page_shift) : 0;
     unsigned char* const pool = (unsigned char*)(is_v ? a.v : a.k);
     if constexpr (OUT == PS_SCALED) {
@@ -170,6 +170,7 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
         }
         e = min(e, PAGED_SCALE_MAX);
         unscale = pow2f(-e);
+        if (e == PAGED_SCALE_MAX) most_code = PAGED_SCALE_MAX_CODE;
         if (lane == 0) *scale = pow2f(e);
       }
     }
@@ -213,7 +214,8 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
         *(u32x4*)(to + sub * EPL) = o;
       } else if constexpr (EPL == 8) {
         *(uint2*)(pool + (row0 + t) * D + sub * OUT_BYTES) =
-            make_uint2(codes4(x[0] * unscale, x[1] * unscale, x[2] * unscale, x[3] * unscale), codes4(x[4] * unscale, x[5] * unscale, x[6] * unscale, x[7] * unscale));
+            make_uint2(codes4(x[0] * unscale, x[1] * unscale, x[2] * unscale, x[3] * unscale, most_code),
+                       codes4(x[4] * unscale, x[5] * unscale, x[6] * unscale, x[7] * unscale, most_code));
       }
     }
   };

@@ -1,0 +1,132 @@
+"""The ends of the scales' range over the paged cache (include/qp_paged.h).
+
+At a scale of 2^120 codes beyond 240 would stand for more than f32 and bf16 hold: appends saturate there, and such codes, where a
+caller's pool has them, are infinities like those of a bf16 pool. Tolerances are those of test_gpu_paged.py and
+test_gpu_paged_rope_window.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as P
+from paper_2505_16175_amd import binding as B
+from paper_2505_16175_amd.workload import to_f64
+from test_gpu_paged import DEV, L7, L72, Scene, check_plain
+from test_gpu_paged_rope_window import SCALED, SECTION, attend, i32, plain, scaled_pool
+
+pytestmark = pytest.mark.gpu
+TOP = 240 * 2.0 ** 120                                            # 1.875 * 2^127
+
+
+def pool_of(sc):
+    return dict(sc.pool(), k_scale=to_f64(sc.cache.k_scale), v_scale=to_f64(sc.cache.v_scale))
+
+
+@pytest.mark.parametrize("rope", [False, True])
+@pytest.mark.parametrize("layout,lens,new", [(L7, [70, 16], [3, 16]), (L72, [100, 300], [37, 1])])
+def test_the_largest_values_are_stored_finite(layout, lens, new, rope):
+    """bf16's largest, some that just do and just do not fit, infinities and NaN, in blocks of their own and behind entries of ordinary size."""
+    sc = scaled_pool(Scene(layout, 16, lens, new, seed=sum(lens)), seed=1, spread=2)
+    g = torch.Generator().manual_seed(2)
+    kv = torch.randn(2, sc.n_rows, sc.h_kv, sc.d, generator=g)
+    kv[:, :, 0] *= 2.0 ** 126
+    kv = kv.to(torch.bfloat16)
+    most = torch.finfo(torch.bfloat16).max
+    for c, x in enumerate((most, -most, 1.75 * 2.0 ** 127, 1.7578125 * 2.0 ** 127, -1.875 * 2.0 ** 127, 1.9375 * 2.0 ** 127, -1.9453125 * 2.0 ** 127,
+                           float("inf"), float("-inf"), float("nan"))):
+        kv[:, sc.starts[0]::2, 1, 3 * c] = x
+        kv[:, sc.starts[0]::2, 1, 64 + 3 * c] = x if c % 2 else -x  # where both turn by 45 degrees the sum is sqrt(2) times as large
+    k, v = kv.to(DEV)
+    pos = torch.arange(sc.n_rows, dtype=torch.int32)
+    before = pool_of(sc)
+    axes = torch.randint(0, 1000, (3, sc.n_rows), generator=g, dtype=torch.int32)
+    turned = to_f64(k)
+    if rope:
+        with np.errstate(invalid="ignore"):
+            turned = P.turn(turned, axes.numpy(), 1e6, SECTION[128])
+        B.paged_append_rope(sc.layout, sc.cache, sc.batch, k, v, pos.to(DEV), B.PagedRope(sc.layout, axes.to(DEV), 1e6, SECTION[128]))
+    else:
+        B.paged_append(sc.layout, sc.cache, sc.batch, k, v, pos.to(DEV))
+    torch.cuda.synchronize()
+    want = P.append_scaled(turned, to_f64(v), to_f64(k), pos[:, None].expand(-1, sc.h_kv).numpy(), before, sc.oracle_batch, 316.0 if rope else 448.0)
+    got = pool_of(sc)
+    live = torch.zeros(sc.cache.c.n_pages, 16, dtype=torch.bool)
+    for s in range(len(lens)):
+        j = torch.arange(lens[s])
+        live[sc.table[s].long()[j // 16], j % 16] = True
+    live = live[:, None].expand(-1, sc.h_kv, -1).numpy()
+    for name in ("k", "v"):
+        assert (want[name + "_scale"] == 2.0 ** 120).any()
+        np.testing.assert_array_equal(got[name + "_scale"], want[name + "_scale"], err_msg=name)
+        with np.errstate(invalid="ignore"):
+            size = np.abs(P.dequantised(got)[name])[live]
+        assert (size[~np.isnan(size)] <= TOP).all(), f"{name}: codes that stand for infinities"
+        if name == "v" or not rope:
+            np.testing.assert_array_equal(got[name], want[name], err_msg=name)
+    if rope:                                                      # one code apart where a turned value lies next to the middle between two
+        finite = np.isfinite(turned).all()
+        assert not finite                                         # the planted ones
+        new_here = np.zeros_like(live)
+        for s in range(len(lens)):
+            j = np.arange(lens[s] - new[s], lens[s])
+            new_here[sc.table[s].numpy()[j // 16], :, j % 16] = True
+        assert np.array_equal(np.isnan(got["k"][new_here]), np.isnan(want["k"][new_here]))
+        off = np.abs(got["k"] - want["k"])[new_here]
+        step = np.maximum(2.0 ** -3 * np.abs(want["k"][new_here]), 2.0 ** -9)
+        assert (off[~np.isnan(off)] <= step[~np.isnan(off)]).all()
+
+
+@pytest.mark.parametrize("made_by", ["append", "caller"])
+@pytest.mark.parametrize("new,window", [(1, None), (4, None), (4, (40, 3)), (40, None), (40, (64, 5))])
+def test_the_largest_values_do_not_reach_rows_that_do_not_see_them(new, window, made_by):
+    """A sequence's last entry holds bf16's largest values, stored by an append, or codes of 448 at the largest scale, which are infinities:
+    the rows before it are as if it was not there."""
+    lens = [230, 97]                                              # last entries at 5 and 0 of their blocks: with others, and alone
+    sc = scaled_pool(Scene(L7, 16, lens, [new, new], seed=new), seed=3, spread=0)
+    huge = []
+    for s, n in enumerate(lens):
+        page, block = int(sc.table[s, (n - 1) // 16]), (n - 1) // 16 * 16
+        for h in (0, 2):
+            if made_by == "append":
+                rows = torch.zeros(n - block, 1, 128, dtype=torch.bfloat16)
+                rows[-1, 0, 3], rows[-1, 0, 70] = torch.finfo(torch.bfloat16).max, -torch.finfo(torch.bfloat16).max
+                one = B.make_layout(1, 1, 128, "bf16")
+                pool = B.PagedCache(one, 1, 16, fmt=SCALED)
+                B.paged_append(one, pool, B.PagedBatch(i32([[0]]), i32([n - block]), i32([0, n - block]), n - block), rows.to(DEV), rows.to(DEV),
+                               torch.zeros(n - block, dtype=torch.int32, device=DEV))
+                torch.cuda.synchronize()
+                assert pool.v_scale.item() == 2.0 ** 120
+                sc.cache.v.view(torch.uint8)[page, h] = pool.v.view(torch.uint8)[0, 0]
+            else:
+                sc.cache.v.view(torch.uint8)[page, h] = 0
+                sc.cache.v.view(torch.uint8)[page, h, (n - 1) % 16, 3], sc.cache.v.view(torch.uint8)[page, h, (n - 1) % 16, 70] = 0x7e, 0xfe
+            sc.cache.v_scale[page, h] = 2.0 ** 120
+            huge.append((s, h))
+    want = plain(sc, *(window or (None,)))
+    for ws in ("full", None):
+        out, lse = attend(sc, *(window or (None,)), ws=ws)
+        for s, h in huge:
+            row, heads = sc.starts[s] + new - 1, slice(7 * h, 7 * h + 7)
+            seen = out[row, heads][:, [3, 70]]
+            if made_by == "caller":
+                assert not torch.isfinite(seen).any()
+            out[row, heads] = want[0][row, heads].to(out.dtype)   # the row that sees it: what a sum of them holds is not looked at here
+        check_plain(sc, out, lse, want, f"{new} {window} {made_by}")
+
+
+def test_a_row_that_sees_the_largest_value_has_it():
+    """One entry and its row, one value in the middle of zeros: the softmax's only weight is 1."""
+    L = B.make_layout(4, 2, 128, "bf16")
+    for rows, n in ((1, 1), (20, 20)):                            # few rows, and a tile (40 stacked rows)
+        cache = B.PagedCache(L, 4, 16, fmt=SCALED)
+        batch = B.PagedBatch(i32([[2, 0]]), i32([n]), i32([0, rows]), rows)
+        v = torch.zeros(rows, 2, 128, dtype=torch.bfloat16, device=DEV)
+        v[0, :, 5], v[0, :, 6] = torch.finfo(torch.bfloat16).max, -1.75 * 2.0 ** 127
+        q = torch.zeros(rows, 4, 128, dtype=torch.bfloat16, device=DEV)
+        B.paged_append(L, cache, batch, torch.zeros_like(v), v, torch.zeros(rows, dtype=torch.int32, device=DEV))
+        out = torch.zeros_like(q)
+        B.paged_attend(L, cache, batch, q, out)
+        torch.cuda.synchronize()
+        assert (out[0, :, 5].double() == TOP).all() and (out[0, :, 6].double() == -1.75 * 2.0 ** 127).all() and (out[0, :, :5] == 0).all()
+        count = torch.arange(1, rows + 1, device=DEV, dtype=torch.float64)[:, None]
+        for c, x in ((5, TOP), (6, -1.75 * 2.0 ** 127)):          # the mean over the entries so far: the value over their number
+            assert ((out[:, :, c].double() - x / count).abs() <= (2.0 ** -8 + 2.0 ** -14) * abs(x) / count).all()

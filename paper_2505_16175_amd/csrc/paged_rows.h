@@ -90,9 +90,10 @@ __device__ __forceinline__ void rows_load_k(const unsigned char* base, int l16, 
   for (int u = 0; u < RowsLayout<E, D>::KL; ++u) k[u] = *(const pr_u32x4*)(base + (at + rows_k_byte<E, D>(u, g)));
 }
 
-// Products of 16 keys (k) with 16 rows (q): result rows are query rows, columns keys.
+// Products of 16 keys (k, codes times scale) with 16 rows (q): result rows are query rows, columns keys. The scale goes into the widening: codes' own
+// products with a query may exceed f32 where the keys' do not.
 template <typename E, int D>
-__device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout<E, D>::KL], const pr_u32x4 (&q)[RowsLayout<E, D>::QF]) {
+__device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout<E, D>::KL], const pr_u32x4 (&q)[RowsLayout<E, D>::QF], float scale) {
   using L = RowsLayout<E, D>;
   pr_f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if constexpr (L::F32) {
@@ -104,7 +105,7 @@ __device__ __forceinline__ pr_f32x4 rows_products(const pr_u32x4 (&k)[RowsLayout
 #pragma unroll
     for (int st = 0; st < L::QF; ++st) {
       pr_u32x4 raw;
-      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1]);
+      if constexpr (L::F8) raw = pr_widen8(k[st >> 1][2 * (st & 1)], k[st >> 1][2 * (st & 1) + 1], scale);
       else raw = k[st];
       s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8, q[st]), __builtin_bit_cast(pr_bf16x8, raw), s, 0, 0, 0);
     }

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
   const int mask = (1 << a.page_shift) - 1;
 
   pr_u32x4 k[KT][L::KL];
-  float scale[KT];  // of the tiles' codes: their products with the queries are multiplied, exactly, instead
+  float scale[KT];  // of the tiles' codes
   int page[KT];
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
@@ -98,10 +98,10 @@ __global__ __launch_bounds__(PW_NW * 64) void paged_weigh_kernel(PagedArgs a, co
     const bool whole = __all(all);
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      const pr_f32x4 st = rows_products<E, D>(k[t], qf);
+      const pr_f32x4 st = rows_products<E, D>(k[t], qf, scale[t]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(st[r], L::SCALED ? c2 * scale[t] : c2, neg[r]));
+        const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[r]));
         w[t] += whole || key0 + 16 * t + l16 <= lim[r] ? p : 0.f;
       }
     }
@@ -200,14 +200,14 @@ __global__ __launch_bounds__(PW_NW * 64, (RT == 1 ? 4 : 3)) void weigh_stream_ke
     float w = 0.f;
 #pragma unroll
     for (int t = 0; t < L::TILES; ++t) {
-      float sum = 0.f, c = c2;
-      if constexpr (L::SCALED) c *= __uint_as_float((unsigned)__builtin_amdgcn_readlane(__float_as_uint(b.scales), t));
+      float sum = 0.f, scale = 1.f;
+      if constexpr (L::SCALED) scale = __uint_as_float((unsigned)__builtin_amdgcn_readlane(__float_as_uint(b.scales), t));
 #pragma unroll
       for (int y = 0; y < RT; ++y) {
-        const pr_f32x4 st = rows_products<E, D>(b.k[t], qf[y]);
+        const pr_f32x4 st = rows_products<E, D>(b.k[t], qf[y], scale);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c, neg[y][r]));
+          const float p = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg[y][r]));
           sum += whole || key0 + 16 * t + l16 <= lim[y][r] ? p : 0.f;
         }
       }

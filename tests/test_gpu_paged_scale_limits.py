@@ -10,7 +10,7 @@ import torch
 from oracle import paged_oracle as P
 from paper_2505_16175_amd import binding as B
 from paper_2505_16175_amd.workload import to_f64
-from test_gpu_paged import DEV, L7, L72, Scene, check_plain
+from test_gpu_paged import DEV, L7, L72, U, Scene, check_plain
 from test_gpu_paged_rope_window import SCALED, SECTION, attend, i32, plain, scaled_pool
 
 pytestmark = pytest.mark.gpu
@@ -130,3 +130,37 @@ def test_a_row_that_sees_the_largest_value_has_it():
         count = torch.arange(1, rows + 1, device=DEV, dtype=torch.float64)[:, None]
         for c, x in ((5, TOP), (6, -1.75 * 2.0 ** 127)):          # the mean over the entries so far: the value over their number
             assert ((out[:, :, c].double() - x / count).abs() <= (2.0 ** -8 + 2.0 ** -14) * abs(x) / count).all()
+
+
+@pytest.mark.parametrize("layout,lens,new", [(L7, [200, 90], 1), (L7, [200, 90], 4), (L7, [200, 90], 40), ((1030, 1030, 128, "bf16"), [50], 33)])
+def test_weigh_with_small_scales_and_large_queries(layout, lens, new):
+    """Codes' own products with such queries exceed what f32 holds; the keys' do not."""
+    sc = Scene(layout, 16, lens, [new] * len(lens), seed=new, fp8=True)
+    shape = (sc.cache.c.n_pages, sc.h_kv, 1)
+    g = torch.Generator().manual_seed(7)
+    sc.cache.k.copy_((sc.cache.k.float() * 100).clamp(-448, 448).to(torch.float8_e4m3fn))
+    sc.cache = B.PagedCache(sc.layout, shape[0], 16, fmt=SCALED, k=sc.cache.k, v=sc.cache.v, pos=sc.cache.pos, weight=sc.cache.weight,
+                            k_scale=torch.exp2(-117 + torch.randint(0, 2, shape, generator=g).float()).to(DEV), v_scale=torch.ones(shape, device=DEV))
+    q = sc.q.float() * 2.0 ** 120
+    q[:, :, ::2] *= 2.0 ** -12
+    q[:, ::3] *= 2.0 ** -4                                        # logits of size 100 and 1,000
+    sc.q = q.to(torch.bfloat16)
+    codes = torch.nan_to_num(sc.cache.k.float()).abs().amax().item()
+    assert float(sc.q.float().abs().max()) * codes > 2.0 ** 128
+    values_pool = P.dequantised(pool_of(sc))
+    _, wl, _, size = P.attend(to_f64(sc.q), values_pool, sc.oracle_batch, sc.scale)
+    if layout is L7:
+        _, lse = attend(sc)
+        assert torch.isfinite(lse[:, sc.starts[0]:sc.starts[-1]]).all()
+    else:                                                         # more heads than the tiles of weighing take
+        lse = torch.tensor(np.nan_to_num(wl), dtype=torch.float32, device=DEV)
+    tol = (sc.d + 16) * U * (np.nan_to_num(size).max() + np.abs(to_f64(lse)).max()) + 2.0 ** -22 + (new * sc.h_q // sc.h_kv + 4) * U
+    for accumulate in (True, False):
+        for ws in (sc.ws, None):
+            before = dict(values_pool, weight=to_f64(sc.cache.weight))
+            B.paged_weigh(sc.layout, sc.cache, sc.batch, sc.q.to(DEV), lse, accumulate, ws)
+            torch.cuda.synchronize()
+            want, added = P.weigh(to_f64(sc.q), to_f64(lse), before, sc.oracle_batch, sc.scale, accumulate)
+            got = to_f64(sc.cache.weight)
+            assert np.isfinite(got).all()
+            assert (np.abs(got - want) <= added * np.expm1(tol) + 2 * U * np.abs(want) + 1e-37).all()

@@ -54,7 +54,10 @@ __global__ __launch_bounds__(PS_THREADS, D * sizeof(T) > 256 ? 3 : 4) void paged
   constexpr int HALF = D / 2, LPR = D / EPL;        // lanes per row
   constexpr int TOKENS = 64 / LPR, PASSES = PS_BLOCK / TOKENS;
   constexpr int OUT_BYTES = OUT == PS_SAME ? 16 : EPL;
-  __shared__ float lds_cos[ROPE ? PS_BLOCK : 1][HALF], lds_sin[ROPE ? PS_BLOCK : 1][HALF];
+  // read 16 bytes at a time
+  __shared__ __attribute__((aligned(16))) float lds_cos[ROPE ? PS_BLOCK : 1][HALF];
+  __shared__ __attribute__((aligned(16))) float lds_sin[ROPE ? PS_BLOCK : 1][HALF];
+  static_assert(__alignof__(lds_cos) >= 16 && __alignof__(lds_sin) >= 16 && HALF * sizeof(float) % 16 == 0, "vector reads of the angles");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int unit = blockIdx.x / groups, group = blockIdx.x - unit * groups;

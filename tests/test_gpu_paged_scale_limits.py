@@ -1,4 +1,4 @@
-"""The ends of the scales' range over the paged cache (include/qp_paged.h).
+"""The ends of the scales' range over the paged cache (include/qp_paged.h), and windows within the limits that a batch states.
 
 At a scale of 2^120 codes beyond 240 would stand for more than f32 and bf16 hold: appends saturate there, and such codes, where a
 caller's pool has them, are infinities like those of a bf16 pool. Tolerances are those of test_gpu_paged.py and
@@ -10,7 +10,7 @@ import torch
 from oracle import paged_oracle as P
 from paper_2505_16175_amd import binding as B
 from paper_2505_16175_amd.workload import to_f64
-from test_gpu_paged import DEV, L7, L72, U, Scene, check_plain
+from test_gpu_paged import DEV, L7, L72, TINY, U, Scene, check_plain
 from test_gpu_paged_rope_window import SCALED, SECTION, attend, i32, plain, scaled_pool
 
 pytestmark = pytest.mark.gpu
@@ -164,3 +164,53 @@ def test_weigh_with_small_scales_and_large_queries(layout, lens, new):
             got = to_f64(sc.cache.weight)
             assert np.isfinite(got).all()
             assert (np.abs(got - want) <= added * np.expm1(tol) + 2 * U * np.abs(want) + 1e-37).all()
+
+
+@pytest.mark.parametrize("layout,fmt", [(L7, "same"), (TINY, "same"), (L7, "scaled")])
+def test_windowed_rows_within_the_limits_are_right(layout, fmt):
+    """Lengths and rows that the device states wrongly: the rows that the batch's limits leave see the entries that they leave, and the others
+    stay as they were."""
+    sc = Scene(layout, 16, [60, 100], [3, 2], seed=5)
+    if fmt == "scaled":
+        scaled_pool(sc)
+    q, r = sc.q.to(DEV), sc.h_q // sc.h_kv
+    pool = pool_of(sc) if fmt == "scaled" else sc.pool()
+    if fmt == "scaled":
+        with np.errstate(invalid="ignore"):
+            pool = P.dequantised(pool)
+    q64 = to_f64(sc.q)
+    for starts in ([2, 5, 7], [-7, 3, 2 ** 31 - 1], [5, 2, 7], [2 ** 31 - 1, -2 ** 31, 4]):
+        for lens in ([2 ** 31 - 1, -5], [-2 ** 31, 47], [49, 48]):
+            batch = B.PagedBatch(sc.table.to(DEV), i32(lens), i32(starts), sc.n_rows, max_new=3, max_len=48)
+            for window, n_sink in ((5, 2), (2 ** 31 - 1, 0), (1, 2 ** 31 - 1), (20, 0)):
+                for ws in (sc.ws, None):
+                    out, lse = torch.full_like(q, 7.0), torch.full((sc.h_q, sc.n_rows), 7.0, device=DEV)
+                    B.paged_attend_window(sc.layout, sc.cache, batch, window, n_sink, q, out, lse, ws)
+                    torch.cuda.synchronize()
+                    got, gl, owned = to_f64(out), to_f64(lse), set()
+                    for s in range(2):
+                        length = min(max(lens[s], 0), 48)
+                        r0 = min(max(starts[s], 0), sc.n_rows)
+                        count = min(max(starts[s + 1], r0), sc.n_rows) - r0
+                        for i in range(min(count, 3)):
+                            owned.add(r0 + i)
+                            p = length - count + i
+                            j = np.arange(max(p + 1, 0))
+                            j = j[(j > p - window) | (j < n_sink)]
+                            page, slot = sc.table[s].numpy()[j // 16], j % 16
+                            for qh in range(sc.h_q):
+                                if len(j) == 0:
+                                    assert (got[r0 + i, qh] == 0).all() and np.isneginf(gl[qh, r0 + i])
+                                    continue
+                                k, v = pool["k"][page, qh // r, slot], pool["v"][page, qh // r, slot]
+                                x = sc.scale * (k @ q64[r0 + i, qh])
+                                w = np.exp(x - x.max())
+                                z = x.max() + np.log(w.sum())
+                                w /= w.sum()
+                                size = sc.scale * (np.abs(k) @ np.abs(q64[r0 + i, qh])).max() + np.abs(x).max()
+                                e = (sc.d + 16) * U * size + 2.0 ** -22
+                                tol = sc.h * np.abs(w @ v) + (w @ np.abs(v)) * (2 * e + (0 if sc.h == U else 2.0 ** -16) + 2.0 ** -15) + 1e-30
+                                assert (np.abs(got[r0 + i, qh] - w @ v) <= tol).all(), (starts, lens, window, r0 + i, qh)
+                                assert abs(gl[qh, r0 + i] - z) <= 2 * e + 2.0 ** -16 + 4 * U * abs(z)
+                    rest = [row for row in range(sc.n_rows) if row not in owned]
+                    assert (got[rest] == 7.0).all() and (gl[:, rest] == 7.0).all()

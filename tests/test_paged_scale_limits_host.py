@@ -1,8 +1,10 @@
-"""The ends of the scales' range over the paged cache, without a GPU."""
+"""The ends of the scales' range and refusals of 8-bit pools, without a GPU."""
 import numpy as np
+import pytest
 import torch
 
 from oracle import paged_oracle as P
+from test_paged_rope_window_host import ALL, UNS, _call
 
 
 def test_oracle_saturates_where_codes_would_be_infinities():
@@ -19,3 +21,11 @@ def test_oracle_saturates_where_codes_would_be_infinities():
     top = np.array([[[1.75 * 2.0 ** 127, 1.0, 0.0, 0.0]]])        # the largest that 448 codes hold
     p = P.append_scaled(top, top, top, np.array([[7]]), p, dict(table=[[0]], lens=[1], row_start=[0, 1]), 448.0)
     assert p["v_scale"].item() == 2.0 ** 119 and p["v"][0, 0, 0, 0] == 448.0
+
+
+@pytest.mark.parametrize("change", [dict(dtype="f32"), dict(d=64, section=(8, 12, 12)), dict(dtype="f32", d=64, section=(8, 12, 12))])
+def test_8_bit_pools_of_other_layouts_are_refused(change):
+    if torch.cuda.is_available():
+        pytest.skip("calls that are not refused would run over made-up addresses")
+    got = _call(format=1, k_scale=None, v_scale=None, **change)
+    assert {got[name] for name in ALL} == {UNS}

@@ -31,7 +31,10 @@
  * 448: keys of channels with large offsets saturate. Codes are floating-point themselves, so a finer scale would not make them more exact; a power of two
  * is exact wherever it is applied. An append gives a block the least scale that holds its finite values (infinities saturate, NaN stays) and never
  * a smaller one than the block's earlier entries have; where it grows, their codes are divided with it, exactly down to 2^-6 of the new
- * scale and rounded below. Entries that qp_paged_evict moves join blocks of new neighbours, whose scale is the largest of theirs, their codes divided in the same way.
+ * scale and rounded below. So an append to a block that is partly full may write entries that were there before it, which with the other formats it never
+ * does: sequences that share such a page have them rounded too, and a call on another stream that reads them meanwhile races with it (share pages up to a
+ * multiple of 16 entries, and go on in a page of one's own). Tokens that are taken back, by a smaller len, leave their block's scale and its codes as they had
+ * become; a block that is begun anew, from its first entry, has no past. Entries that qp_paged_evict moves join blocks of new neighbours, whose scale is the largest of theirs, their codes divided in the same way.
  */
 #ifndef QP_PAGED_H_
 #define QP_PAGED_H_
@@ -73,7 +76,8 @@ typedef struct {
 } qp_paged_batch;
 
 /* Workspace that every call below accepts for batches of these sizes (256-byte aligned where it is handed over): partial
- * results of qp_paged_attend (128 MiB at most) and qp_paged_weigh, the selection of qp_paged_evict with `keep` (0: none). 0 on
+ * results of qp_paged_attend (128 MiB at most) and qp_paged_weigh, the selection of qp_paged_evict with `keep` (0: none). Counted without
+ * a window: qp_paged_attend_window would deal short windows, or those of many sequences, to more workgroups if it got more (up to the same 128 MiB). 0 on
  * bad arguments. */
 size_t qp_paged_workspace_bytes(const qp_layout* layout, int32_t n_seqs, int32_t n_rows, int32_t max_new, int32_t max_len,
                                 int32_t keep);
@@ -152,7 +156,7 @@ qp_status qp_paged_evict(const qp_layout* layout, const qp_paged_cache* cache, c
                          int32_t n_first, int32_t n_last, const int32_t* to_table, int32_t to_pages, int32_t* to_len,
                          int32_t* kept_or_null, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* How qp_paged_attend would lay out a call (host arithmetic only). Few rows: `shares` workgroups of every KV head divide the entries
+/* How qp_paged_attend (without a window) would lay out a call (host arithmetic only). Few rows: `shares` workgroups of every KV head divide the entries
  * of all sequences evenly among them (0: a workgroup per sequence, head and row tile, no scratch). Chunks over bf16 heads of 128:
  * key_chunks of chunk_entries of every sequence (1: no scratch). */
 typedef struct {

@@ -653,6 +653,8 @@ class PagedRope:
             raise ValueError("axes: expected int32 [3][n_rows] or [n_rows]")
         if axes.get_device() < 0 or not axes.is_contiguous():
             raise ValueError("axes: expected a contiguous tensor on the GPU")
+        if any(x >> 31 not in (0, -1) for x in section):
+            raise ValueError("section: expected 32-bit numbers")
         self.axes, self.n_rows, self.device_index, self.head_dim = axes, axes.shape[-1], axes.get_device(), layout.head_dim
         self.c = qp_paged_rope(axes.data_ptr(), axes.shape[1] if axes.dim() == 2 else 0, theta, (ctypes.c_int32 * 3)(*section))
         self.ref = ctypes.byref(self.c)
@@ -720,6 +722,8 @@ def paged_attend(layout, cache: PagedCache, batch: PagedBatch, q, out, lse=None,
 def paged_attend_window(layout, cache: PagedCache, batch: PagedBatch, window, n_sink, q, out, lse=None, workspace=None):
     """paged_attend in which the row that is entry p sees the entries j <= p with j > p - window or j < n_sink."""
     here = _same_gpu(layout, cache, batch)
+    if window >> 31 not in (0, -1) or n_sink >> 31 not in (0, -1):   # ctypes would drop the upper bits
+        raise ValueError("window, n_sink: expected 32-bit numbers")
     dt, shape = _layout_dtype(layout), (batch.n_rows, layout.n_q_heads, layout.head_dim)
     wp, wb = _scratch(workspace, here)
     st = lib().qp_paged_attend_window(ctypes.byref(layout), cache.ref, batch.of(cache), window, n_sink, _dense(q, dt, shape, "q", here),

@@ -214,3 +214,17 @@ def test_windowed_rows_within_the_limits_are_right(layout, fmt):
                                 assert abs(gl[qh, r0 + i] - z) <= 2 * e + 2.0 ** -16 + 4 * U * abs(z)
                     rest = [row for row in range(sc.n_rows) if row not in owned]
                     assert (got[rest] == 7.0).all() and (gl[:, rest] == 7.0).all()
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """Their lower bits alone would be a window, a count of first entries or a section of another size."""
+    sc = Scene(TINY, 16, [60], [2], seed=1)
+    q, out = sc.q.to(DEV), torch.full((sc.n_rows, sc.h_q, sc.d), 7.0, device=DEV)
+    for window, n_sink in (((1 << 32) + 5, 2), (5, 1 << 32), (5 - (1 << 32), 0), (5, 1 << 31), (1 << 40, 0)):
+        with pytest.raises(ValueError):
+            B.paged_attend_window(sc.layout, sc.cache, sc.batch, window, n_sink, q, out)
+    with pytest.raises(ValueError):
+        B.PagedRope(sc.layout, torch.zeros(5, dtype=torch.int32, device=DEV), section=((1 << 32) + 8, 12, 12))
+    assert (out == 7.0).all()
+    B.paged_attend_window(sc.layout, sc.cache, sc.batch, 2 ** 31 - 1, 2 ** 31 - 1, q, out)
+    assert not (out[sc.starts[0]:sc.starts[1]] == 7.0).any()

@@ -248,12 +248,11 @@ struct RowsWave {
   // hardly anything else is, count as if they had one.
   __device__ __forceinline__ bool values_not_finite(const Block& b) const {
     constexpr unsigned ONES = L::F32 ? 0x7f800000u : L::F8 ? 0x7f7f7f7fu : 0x7f807f80u, LEAST = L::F32 ? 0x00800000u : L::F8 ? 0x01010101u : 0x00800080u;
-    if constexpr (L::SCALED) {
-#pragma unroll
-      for (int t = 0; t < L::TILES; ++t)
-        if (b.value_scale(t) >= 0x1p120f) return true;
-    }
     unsigned found = 0;
+    if constexpr (L::SCALED) {
+      const int top = max((int)__float_as_uint(b.value_scale(0)), (int)__float_as_uint(b.value_scale(L::TILES - 1)));
+      if (top >= (int)__float_as_uint(0x1p120f)) return true;
+    }
 #pragma unroll
     for (int j = 0; j < L::VK; ++j)
 #pragma unroll

@@ -228,3 +228,65 @@ def test_numbers_beyond_32_bits_are_refused():
     assert (out == 7.0).all()
     B.paged_attend_window(sc.layout, sc.cache, sc.batch, 2 ** 31 - 1, 2 ** 31 - 1, q, out)
     assert not (out[sc.starts[0]:sc.starts[1]] == 7.0).any()
+
+
+@pytest.mark.parametrize("layout,keep,more", [(L7, 75, 5), (L72, 33, 40), (L7, 16, 17)])
+def test_an_evicted_cache_with_scales_goes_on(layout, keep, more):
+    """Entries stored, attended, weighed and cut to a budget that ends inside a block, and the next tokens stored behind them: the block that
+    the move began takes them, its scale grows from what the move gave it. Lengths stay on the device."""
+    h_q, h_kv, d, _ = layout
+    L, g, page, lens = B.make_layout(*layout), torch.Generator().manual_seed(keep), 32, [230, 41]
+    cache = B.PagedCache(L, 30, page, fmt=SCALED)
+    order = torch.randperm(30, generator=g)
+    table, to = order[:16].view(2, 8).int(), order[16:].view(2, 7).int()
+    made = lambda n, size: (size * torch.randn(n, h_kv, d, generator=g)).to(torch.bfloat16)
+    pool = lambda: dict(k=to_f64(cache.k.float()), v=to_f64(cache.v.float()), pos=cache.pos.cpu().numpy(), weight=to_f64(cache.weight),
+                        k_scale=to_f64(cache.k_scale), v_scale=to_f64(cache.v_scale))
+
+    def append(t, length, lens, starts, size):
+        n, before = starts[-1], pool()
+        k, v, pos = made(n, size), made(n, 1 / size), torch.arange(n, dtype=torch.int32)
+        B.paged_append(L, cache, B.PagedBatch(t.to(DEV), length, i32(starts), n), k.to(DEV), v.to(DEV), pos.to(DEV))
+        torch.cuda.synchronize()
+        want = P.append_scaled(to_f64(k), to_f64(v), to_f64(k), pos[:, None].expand(-1, h_kv).numpy(), before,
+                               dict(table=t.tolist(), lens=lens, row_start=starts), 448.0)
+        got = pool()
+        for name in want:
+            np.testing.assert_array_equal(got[name], want[name], err_msg=name)
+
+    append(table, i32(lens), lens, [0, lens[0], sum(lens)], 1.0)
+    length, rows = i32(lens), 2
+    q = torch.randn(2 * rows, h_q, d, generator=g).to(torch.bfloat16).to(DEV)
+    batch = B.PagedBatch(table.to(DEV), length, i32([0, rows, 2 * rows]), 2 * rows, max_new=rows)
+    ws = B.make_paged_workspace(L, batch, keep, page)
+    out, lse = torch.empty_like(q), torch.empty(h_q, 2 * rows, device=DEV)
+    B.paged_attend(L, cache, batch, q, out, lse, ws)
+    B.paged_weigh(L, cache, batch, q, lse, True, ws)
+    torch.cuda.synchronize()
+    before = pool()
+    lists = P.evict(before, table.tolist(), lens, keep, 4, 8)
+    lists = [lists[:h_kv], lists[h_kv:]]
+    B.paged_evict(L, cache, batch, keep, 4, 8, to.to(DEV), length, None, ws)
+    want = P.move_scaled(before, table.tolist(), lists, to.tolist())
+    torch.cuda.synchronize()
+    got = pool()
+    for name in want:
+        np.testing.assert_array_equal(got[name], want[name], err_msg=name)
+    lens = [min(keep, n) for n in lens]
+    assert length.tolist() == lens
+    for size in (30.0, 1e-3):
+        length.add_(more)
+        lens = [n + more for n in lens]
+        append(to, length, lens, [0, more, 2 * more], size)
+    now = P.dequantised(pool())
+    q = torch.randn(2 * more, h_q, d, generator=g).to(torch.bfloat16)
+    batch = B.PagedBatch(to.to(DEV), length, i32([0, more, 2 * more]), 2 * more, max_new=more)
+    numerators = 2.0 ** -8 if B.paged_plan(L, cache, batch, 0)["rows_per_tile"] == 256 else 2.0 ** -16
+    for window, n_sink in ((1 << 20, 0), (20, 3)):
+        out, lse = torch.empty(2 * more, h_q, d, dtype=torch.bfloat16, device=DEV), torch.empty(h_q, 2 * more, device=DEV)
+        B.paged_attend_window(L, cache, batch, window, n_sink, q.to(DEV), out, lse, B.make_paged_workspace(L, batch, 0, page))
+        torch.cuda.synchronize()
+        want, wl, absv, size = P.attend(to_f64(q), now, dict(table=to.tolist(), lens=lens, row_start=[0, more, 2 * more]), 128 ** -0.5, window, n_sink)
+        e = (d + 16) * U * size + 2.0 ** -22
+        assert (np.abs(to_f64(out) - want) <= 2.0 ** -8 * np.abs(want) + absv * (2 * e.T[:, :, None] + numerators + 2.0 ** -15) + 1e-30).all()
+        assert (np.abs(to_f64(lse) - wl) <= 2 * e + 2.0 ** -16 + 4 * U * np.abs(wl)).all()

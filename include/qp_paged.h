@@ -120,7 +120,8 @@ qp_status qp_paged_append_rope(const qp_layout* layout, const qp_paged_cache* ca
  * products and sums; bf16 rows' softmax numerators are rounded to bf16 before the product with V (to two bf16 terms in calls of up to
  * 32 stacked rows, max_new * H_q / H_kv, and over heads of 64), never in the sums behind lse. All rows of a call take the same way, so
  * a row's last bits depend on max_new. What a row does not see does not reach its result, infinities and NaN included; an
- * infinite value that it sees makes its element infinite, or NaN. Logits scale * q.k of
+ * infinite value that it sees makes its element infinite, or NaN. Values are summed in f32, each times a numerator of up to 2^8: where those that a row
+ * sees add up to more than 2^119 in size, its element may be infinite too. Logits scale * q.k of
  * up to 2^28 in size are computed; those below -2^29 weigh nothing, as -infinity does, and a row that sees nothing else is one that sees
  * no entry; of a row with one above 2^28 nothing is promised.
  *   workspace: may be NULL. Where the rows would leave compute units idle, their entries are dealt to several workgroups

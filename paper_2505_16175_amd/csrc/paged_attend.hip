@@ -44,7 +44,7 @@ struct PagedOut {
   int2* info;      // [units]: first share of a unit and the shares that have blocks of it
 };
 
-// Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles fill the registers (with scales 4 of them spill, around
+// Two workgroups per compute unit for heads of 64 and over 8-bit pools, where two row tiles fill the registers (with scales 4 of them spill, 5 in windows, around
 // the loop over the keys). Of bf16 heads of 128 one has the registers to itself: squeezed into half of them its results and
 // addresses spill around the loop, one token over 46,125 entries 29.4 us, not 26. Of f32 heads of 128 too.
 template <typename E, int D>
@@ -401,10 +401,11 @@ static long long merge_blocks(const PagedArgs& a, const PagedPlan& p) {
 }
 
 // Stacked rows above which bf16 heads of 128 take the tile kernel (attend_mfma.hip), and what its 32-bit arithmetic takes. A workgroup
-// for few rows holds 32; more of them take the entries once for each 32. us few rows (before masks went behind a branch there) / tiles, 7B heads, one sequence over 46,125
-// entries: 1 token 26.0 / 29.3, 4 (28 rows) 30.9 / 30.9, 5 45.7 / 31.9, 12 61.9 / 35.8; 72B heads 46.0 / 56.6, 49.7 / 58.3, 77.8 / 59.5,
-// 106.9 / 65.4. Of 16 sequences over up to 9,840 the tiles win later, 7B heads 57.8 / 78.7, 64.8 / 79.9, 8 tokens 75.6 / 82.1, 12
-// 94.1 / 86.4; 72B heads 95.2 / 111.0, 110.4 / 112.4, 135.2 / 116.6; over 8-bit pools of the 7B heads not up to 12 (68.3 / 90.0).
+// for few rows holds 32; more of them take the entries once for each 32. us few rows / tiles, 1, 4, 5, 8 and 12 tokens (of the 7B heads 28 rows are 4, of
+// the 72B ones 32), one sequence over 46,125 entries: 7B heads, bf16 26.4 / 29.3, 29.6 / 30.5, 40.4 / 31.1, 41.8 / 32.3, 57.2 / 34.4, 8-bit 21.7 / 29.6,
+// 25.0 / 31.1, 28.3 / 31.9, 29.7 / 33.1, 38.5 / 35.2; 72B heads, bf16 44.4 / 55.5, 47.8 / 57.4, 71.4 / 58.4, 72.9 / 60.7, 101 / 64.5, 8-bit 26.9 / 55.7,
+// 32.5 / 57.6, 40.3 / 59.5, 42.0 / 61.7, 60.0 / 65.6. Of 16 sequences over up to 9,840 and over 8-bit pools, with scales or without, the tiles win later
+// than the rule has it: 12 tokens of the 7B heads 76.5 / 81.7, 8-bit 47.1 / 88.6, with scales 52.3 / 91.2, of the 72B heads 140 / 102, 82.3 / 108, 91.5 / 111.
 constexpr long long PT_FROM_ROWS = 32, PT_MOST_ROWS = 1 << 26;
 
 PagedPlan plan_paged_attend(const PagedArgs& a, int dtype, int d, size_t scratch_bytes) {
